@@ -194,6 +194,85 @@ int nsa_sel_bwd_gated(const nsa_sel_shape* shape, const void* Q, const void* K, 
 int nsa_sel_select_blocks(const nsa_sel_shape* shape, const float* scores, int64_t score_stride,
                           const int32_t* cu_seqlens, int32_t n_sink, int32_t n_local, int32_t* idx, void* stream);
 
+/* ---- Serving from a paged cache ------------------------------------------------------------------------------------
+ * After a prompt a model answers token by token: keys and values lie in a cache of pages, and a call brings a few new
+ * tokens of each of many sequences.  The three calls below are that step: nsa_sel_cache_append writes the new keys and
+ * values and rotates keys and queries by their places, nsa_sel_select_blocks_cached picks the blocks, and
+ * nsa_sel_cache_attention attends.  Forward only.  The conventions above hold, and:
+ *   - K and V pages are [n_pages, hkv, page, d], bf16 or e4m3 (OCP, no infinities).  In e4m3 every (page, KV head) has
+ *     one fp32 scale, a power of two between 2^-100 and 2^119, in k_scale / v_scale [n_pages, hkv]: a stored value stands
+ *     for value * scale.  The kernels read a scale's exponent alone.
+ *   - table is int32 [nseq, max_pages]: column c of row s names the page that holds the places [c * page, (c + 1) * page)
+ *     of sequence s.  Entries outside [0, n_pages), and columns past max_pages, are no pages: nothing is written to them
+ *     and their keys are invisible.  Sequences may share pages that none of them is appending to.
+ *   - kv_len is int32 [nseq]: tokens of each sequence INCLUDING the new ones.  The new tokens of all sequences are packed
+ *     like a training batch: cu_seqlens int32 [nseq + 1] holds their starts; NULL means one new token for each sequence
+ *     (n_tokens == nseq).  New token i of n of sequence s has place kv_len[s] - n + i; tokens of negative place are not
+ *     appended and see nothing.  Tokens before cu_seqlens[0] and from cu_seqlens[nseq] on belong to no sequence: their rows
+ *     of every output are left as they were.  Sequences may have no new token.
+ *   - What lies in a page behind a sequence's last token is never looked at, whatever it holds. */
+#define NSA_SEL_CACHE_BF16 0
+#define NSA_SEL_CACHE_E4M3 1
+
+typedef struct {
+  int32_t n_tokens;       /* new tokens: rows of Q; >= 0                                                          */
+  int32_t nseq;           /* sequences, >= 1 (0 with n_tokens == 0)                                               */
+  int32_t hq, hkv;        /* query / KV heads; g = hq / hkv must be an integer in [1, 8]                          */
+  int32_t d;              /* head dimension; 128 only                                                             */
+  int32_t dtype;          /* NSA_SEL_CACHE_BF16 or NSA_SEL_CACHE_E4M3                                             */
+  int32_t page;           /* tokens per page: 16, 32, 64, 128 or 256                                              */
+  int32_t n_pages;        /* pages of the cache                                                                   */
+  int32_t max_pages;      /* columns of table; max_pages * page <= 2^30                                           */
+  int32_t block;          /* attention: tokens per selected block, 64 or 128 (ignored with topk = 0)              */
+  int32_t topk;           /* attention: columns of idx, 1..32; 0: no selection, every key (of the window)         */
+  int32_t window;         /* attention: 0, or key u is visible to the token at place p only if u > p - window     */
+  float   scale;          /* attention: softmax scale; <= 0 selects 1/sqrt(d)                                     */
+} nsa_sel_cache_shape;
+
+/* Appends K and V [n_tokens, hkv, d] bf16 to the cache, K rotated by its tokens' places, and writes the rotated
+ * queries.  Q, K, V have q_stride, k_stride, v_stride elements between tokens (a multiple of 8, at least heads * d: they
+ * may be slices of one projection); the heads of a token are contiguous.
+ *   inv_freq is DEVICE double [rot / 2], radians per place; rot, a multiple of 16 up to d, is the number of leading channels that
+ *   turn (0: none, inv_freq may be NULL).  Pair i is channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved != 0.  Angles
+ *   are formed in 64 bits.
+ *   Q may be NULL (then Q_out too); Q_out is bf16 [n_tokens, hq, d] and may be Q itself if q_stride = hq * d.
+ *   K_out may be NULL; else it gets the rotated keys, bf16 [n_tokens, hkv, d], for the prompt's own attention (it may be
+ *   K itself if k_stride = hkv * d).
+ * bf16: one rounding of the rotated value.  e4m3: the scale of a (page, head) is the least 2^e with |x| <= 448 * 2^e for all
+ * new values x of the call in that page; in a page that held earlier tokens of the sequence it never shrinks, and where it
+ * grows they are rounded again to the new scale (exact except for values below 2^-14 of it).  Values then are rounded to the
+ * nearest; infinities and NaN are stored as NaN and do not count for the scale, and what the largest scale cannot hold is
+ * stored as 448 * 2^119.  A page's other slots are left as they are.  Pages that are written must not be named twice in
+ * the call. */
+int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                         const void* V, int64_t v_stride, const int32_t* cu_seqlens, const int32_t* kv_len,
+                         const int32_t* table, const double* inv_freq, int32_t rot, int32_t interleaved, void* k_pages,
+                         void* v_pages, float* k_scale, float* v_scale, void* Q_out, void* K_out, void* stream);
+
+/* Bytes of the workspace of nsa_sel_cache_attention for `shape` (0 where the call needs none). */
+int nsa_sel_cache_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes);
+
+/* O and LSE (as nsa_sel_fwd's) of the new tokens over the cache.  Key u is visible to the token at place p if u <= p, u lies
+ * in the window, its page exists and, with topk > 0, its block of `block` tokens is among idx[t, kv head, :] (int32
+ * [n_tokens, hkv, topk], ids local to the sequence; negative ids, blocks that begin after p and repeats are ignored).
+ * topk = 0 takes no idx.  Made for a few new tokens a sequence: tokens of a sequence share reads only without idx.
+ * With gate (DEVICE fp32 [n_tokens, hq]) O receives O_acc + gate * result instead, formed before the one rounding;
+ * O_acc (bf16 like O, may be O itself) may be NULL for zero.  LSE is that of the attention either way.
+ * A row without visible keys gets O = 0 (O_acc with a gate), LSE = -inf; so does one whose visible scores are all -inf.
+ * Results are bit-reproducible and do not depend on the batch a token is in, but for the number of workgroups that share a row. */
+int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, const int32_t* idx, const int32_t* cu_seqlens,
+                            const int32_t* kv_len, const int32_t* table, const void* k_pages, const void* v_pages,
+                            const float* k_scale, const float* v_scale, const float* gate, const void* O_acc, void* O,
+                            float* LSE, void* ws, size_t ws_bytes, void* stream);
+
+/* nsa_sel_select_blocks for the new tokens of cached sequences: the same rule, causal, with the token's place in its
+ * sequence taken from kv_len (cur = place / block, visible blocks 0 .. cur; a negative place sees none).  scores is DEVICE
+ * fp32 [n_tokens, hkv, score_stride] or NULL, idx DEVICE int32 [n_tokens, hkv, topk].  Blocks from score_stride on do not
+ * exist for the call.  Uses shape->n_tokens, nseq, hkv, block and topk; the other fields are ignored. */
+int nsa_sel_select_blocks_cached(const nsa_sel_cache_shape* shape, const float* scores, int64_t score_stride,
+                                 const int32_t* cu_seqlens, const int32_t* kv_len, int32_t n_sink, int32_t n_local,
+                                 int32_t* idx, void* stream);
+
 /* Optional per-kernel timing for benchmarks (not part of the paper's method).  After
  * nsa_sel_profile_enable(capacity > 0) every kernel launch of the calls above is bracketed by a pair of HIP
  * events on the caller's stream, up to `capacity` launches (later ones are not recorded); capacity <= 0 turns

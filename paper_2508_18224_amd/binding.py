@@ -12,6 +12,7 @@ _LIB_PATH = os.path.join(_HERE, "libnsa_sel.so")
 _lib = None
 
 SYMBOLS = ["nsa_sel_workspace_bytes", "nsa_sel_workspace_bytes_min", "nsa_sel_build_index", "nsa_sel_index_view", "nsa_sel_fwd", "nsa_sel_bwd", "nsa_sel_fwd_static", "nsa_sel_fwd_query_outer", "nsa_sel_fwd_gated", "nsa_sel_bwd_gated", "nsa_sel_select_blocks",
+           "nsa_sel_cache_append", "nsa_sel_cache_workspace_bytes", "nsa_sel_cache_attention", "nsa_sel_select_blocks_cached",
            "nsa_sel_profile_enable", "nsa_sel_profile_select", "nsa_sel_profile_collect", "nsa_sel_calibration_copy", "nsa_sel_mfma_probe", "nsa_sel_strerror"]
 
 
@@ -24,6 +25,12 @@ class Shape(C.Structure):
                 ("d", C.c_int32), ("block", C.c_int32), ("topk", C.c_int32), ("causal", C.c_int32),
                 ("scale", C.c_float), ("max_seqlen", C.c_int32), ("window", C.c_int32), ("unit", C.c_int32),
                 ("dense", C.c_int32)]
+
+
+class CacheShape(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("nseq", C.c_int32), ("hq", C.c_int32), ("hkv", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("page", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("block", C.c_int32), ("topk", C.c_int32), ("window", C.c_int32), ("scale", C.c_float)]
 
 
 def lib():
@@ -45,6 +52,11 @@ def lib():
         L.nsa_sel_fwd_gated.argtypes = [C.POINTER(Shape), vp, vp, vp, i32p, i32p, C.c_int, vp, sz, vp, vp, vp, vp, vp, vp, sz, vp]
         L.nsa_sel_bwd_gated.argtypes = [C.POINTER(Shape), vp, vp, vp, vp, vp, vp, vp, i32p, vp, sz, vp, vp, vp, vp, vp, sz, vp]
         L.nsa_sel_select_blocks.argtypes = [C.POINTER(Shape), vp, C.c_int64, i32p, C.c_int32, C.c_int32, i32p, vp]
+        i64 = C.c_int64
+        L.nsa_sel_cache_append.argtypes = [C.POINTER(CacheShape), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, vp]
+        L.nsa_sel_cache_workspace_bytes.argtypes = [C.POINTER(CacheShape), C.POINTER(sz)]
+        L.nsa_sel_cache_attention.argtypes = [C.POINTER(CacheShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.nsa_sel_select_blocks_cached.argtypes = [C.POINTER(CacheShape), vp, i64, vp, vp, C.c_int32, C.c_int32, vp, vp]
         L.nsa_sel_profile_enable.argtypes = [C.c_int]
         L.nsa_sel_profile_select.argtypes = [C.c_uint]
         L.nsa_sel_profile_collect.argtypes = [C.c_int, C.POINTER(C.c_char_p), C.POINTER(C.c_float),
@@ -211,14 +223,35 @@ def nsa_sel_bwd(shape, q, k, v, o, lse, do, cu, index_ws, dq, dk, dv, ws):
 
 
 def select_blocks(scores: torch.Tensor, cu: Optional[torch.Tensor], topk: int, *, block: int = 64,
-                  causal: bool = True, n_sink: int = 1, n_local: int = 2, out: Optional[torch.Tensor] = None):
-    """idx int32 [tokens, hkv, topk] from fp32 scores [tokens, hkv, stride] (nsa_sel_select_blocks)."""
+                  causal: bool = True, n_sink: int = 1, n_local: int = 2, out: Optional[torch.Tensor] = None,
+                  kv_len: Optional[torch.Tensor] = None):
+    """idx int32 [tokens, hkv, topk] from fp32 scores [tokens, hkv, stride] (nsa_sel_select_blocks).
+
+    With kv_len (int32 [sequences], tokens of each cached sequence with its new ones) the rows are the new tokens of cached
+    sequences (nsa_sel_select_blocks_cached, always causal): cu holds the starts of each sequence's new tokens, or is None for one
+    new token each.  Rows of tokens that belong to no sequence are left as `out` has them, and are -1 in a new one."""
     if scores.dtype != torch.float32 or scores.dim() != 3:
         raise NsaSelError("scores must be float32 [tokens, hkv, stride]")
     T, hkv, stride = scores.shape
+    dev = scores.device
+    if kv_len is not None:
+        if not causal:
+            raise NsaSelError("new tokens of cached sequences are selected for causally")
+        nseq = kv_len.numel()
+        if cu is None and nseq != T:
+            raise NsaSelError(f"without cu_seqlens every sequence has one new token: {nseq} lengths for {T} tokens")
+        if out is None:
+            out = torch.empty(T, hkv, topk, dtype=torch.int32, device=dev) if cu is None else torch.full((T, hkv, topk), -1, dtype=torch.int32, device=dev)
+        expect_tensor("scores", scores, torch.float32, (T, hkv, stride), dev)
+        expect_tensor("cu_seqlens", cu, torch.int32, (nseq + 1,), dev, optional=True)
+        expect_tensor("kv_len", kv_len, torch.int32, (nseq,), dev)
+        expect_tensor("out", out, torch.int32, (T, hkv, topk), dev)
+        shape = CacheShape(T, nseq, hkv, hkv, 128, 0, 64, 0, 0, block, topk, 0, 0.0)
+        _launch(lib().nsa_sel_select_blocks_cached, "nsa_sel_select_blocks_cached", dev, C.byref(shape), _ptr(scores), stride, _ptr(cu),
+                _ptr(kv_len), n_sink, n_local, _ptr(out))
+        return out
     nseq = 1 if cu is None else cu.numel() - 1
     shape = Shape(T, nseq, hkv, hkv, 128, block, topk, int(causal), 0.0, 0)
-    dev = scores.device
     if out is None:
         out = torch.empty(T, hkv, topk, dtype=torch.int32, device=dev)
     expect_tensor("scores", scores, torch.float32, (T, hkv, stride), dev)

@@ -1,0 +1,202 @@
+"""A paged cache of keys and values and the calls over it (the nsa_sel_cache_* part of include/nsa_sel.h, which states the rules).  Like
+binding.py this marshals and checks arguments; no arithmetic happens here."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from .binding import CacheShape, NsaSelError, _check, _device, _launch, _ptr, expect_tensor, expect_workspace, lib
+
+_BF16, _F32, _I32, _F64 = torch.bfloat16, torch.float32, torch.int32, torch.float64
+_D = 128
+
+
+def _expect_rows(name: str, t, heads: int, tokens: Optional[int], device) -> None:
+    """bf16 [tokens, heads, 128] whose tokens may lie apart (a slice of one projection) but whose heads may not."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not _BF16 or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != _D:
+        raise NsaSelError(f"{name} must be bfloat16 [tokens, {heads}, {_D}]")
+    if tokens is not None and t.shape[0] != tokens:
+        raise NsaSelError(f"{name} must have {tokens} tokens, got {t.shape[0]}")
+    if t.device != device:
+        raise NsaSelError(f"{name} must live on {device}, got {t.device}")
+    if t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != _D)):
+        raise NsaSelError(f"the heads of a token of {name} must be contiguous")
+    if t.shape[0] > 1 and (t.stride(0) < heads * _D or t.stride(0) % 8):
+        raise NsaSelError(f"the tokens of {name} must be a multiple of 8 values apart, and not overlap")
+    if t.shape[0] > 0 and t.data_ptr() % 16:
+        raise NsaSelError(f"{name} must be 16-byte aligned")
+
+
+def _token_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * _D
+
+
+class PagedCache:
+    """Pages of keys and values, [n_pages, hkv, page, 128] each, in bfloat16 or torch.float8_e4m3fn; in the latter with one power-of-two
+    scale for every (page, KV head).  Which pages a sequence has is the caller's: `table` (int32 [sequences, max_pages], page ids, -1 for
+    none) and `kv_len` (int32 [sequences], lengths INCLUDING the new tokens) go with every call.  The new tokens of all sequences are
+    packed, their starts in `cu` (int32 [sequences + 1]); cu = None: one new token for each sequence.
+
+    A step of a layer is append, selection, attention:
+
+        q, _ = cache.append(k, v, table, kv_len, q=q, inv_freq=inv_freq)
+        idx = select_blocks(scores, None, topk, kv_len=kv_len)
+        o, lse = cache.attention(q, table, kv_len, idx=idx)
+
+    Forward only.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
+    race, as writes to any tensor do."""
+
+    def __init__(self, n_pages: int, hkv: int, *, page: int = 64, dtype: torch.dtype = _BF16, device="cuda:0"):
+        device = _device(device)
+        if dtype not in (_BF16, torch.float8_e4m3fn):
+            raise NsaSelError(f"pages must be bfloat16 or float8_e4m3fn, got {dtype}")
+
+        def zeros():
+            bits = torch.int16 if dtype is _BF16 else torch.uint8
+            return torch.zeros((n_pages, hkv, page, _D), dtype=bits, device=device).view(dtype)
+        scales = (None, None) if dtype is _BF16 else (torch.ones((n_pages, hkv), dtype=_F32, device=device) for _ in range(2))
+        self._set(zeros(), zeros(), *scales)
+
+    @classmethod
+    def from_tensors(cls, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                     v_scale: Optional[torch.Tensor] = None) -> "PagedCache":
+        """A cache in the caller's own tensors."""
+        self = cls.__new__(cls)
+        self._set(k_pages, v_pages, k_scale, v_scale)
+        return self
+
+    def _set(self, k_pages, v_pages, k_scale, v_scale):
+        if not isinstance(k_pages, torch.Tensor) or k_pages.dtype not in (_BF16, torch.float8_e4m3fn) or k_pages.dim() != 4:
+            raise NsaSelError("pages must be bfloat16 or float8_e4m3fn [n_pages, hkv, page, 128]")
+        n_pages, hkv, page, d = k_pages.shape
+        if d != _D or page not in (16, 32, 64, 128, 256) or hkv < 1:
+            raise NsaSelError(f"pages must be [n_pages, hkv, page, {_D}] with 16, 32, 64, 128 or 256 tokens a page, got {tuple(k_pages.shape)}")
+        expect_tensor("k_pages", k_pages, k_pages.dtype, k_pages.shape, k_pages.device)
+        expect_tensor("v_pages", v_pages, k_pages.dtype, k_pages.shape, k_pages.device)
+        e4m3 = k_pages.dtype is not _BF16
+        if e4m3:
+            expect_tensor("k_scale", k_scale, _F32, (n_pages, hkv), k_pages.device)
+            expect_tensor("v_scale", v_scale, _F32, (n_pages, hkv), k_pages.device)
+        elif k_scale is not None or v_scale is not None:
+            raise NsaSelError("bfloat16 pages have no scales")
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.n_pages, self.hkv, self.page, self.device = n_pages, hkv, page, k_pages.device
+        self._dtype = 1 if e4m3 else 0
+        self._pointers = tuple(_ptr(t) for t in (k_pages, v_pages, k_scale, v_scale))
+
+    def _batch(self, tokens: int, table, kv_len, cu) -> Tuple[int, int]:
+        """(sequences, columns of table) after the checks that all calls share."""
+        dev = self.device
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise NsaSelError("table must be int32 [sequences, max_pages]")
+        nseq, max_pages = table.shape
+        expect_tensor("table", table, _I32, (nseq, max_pages), dev)
+        expect_tensor("kv_len", kv_len, _I32, (nseq,), dev)
+        if cu is not None:
+            expect_tensor("cu_seqlens", cu, _I32, (nseq + 1,), dev)
+        elif nseq != tokens:
+            raise NsaSelError(f"without cu_seqlens every sequence has one new token: {nseq} sequences for {tokens} tokens")
+        return nseq, max_pages
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
+               q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+               rotated_k: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+        """Writes k and v (bfloat16 [tokens, hkv, 128]) to the pages, k rotated by its tokens' places, and returns (rotated q or None,
+        rotated k as bfloat16 or None).  q, k, v may be slices whose tokens lie apart.
+
+        inv_freq: float64 [rot / 2], radians per place, rot a multiple of 16 up to 128 leading channels; None rotates nothing.  Pairs are
+        channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved.  rotated_k also returns the rotated keys, for the prompt's own
+        attention.  q_out / k_out take the results (they may be q / k themselves if those are contiguous); rows of tokens that belong to no
+        sequence are left as they are there, and uninitialised otherwise."""
+        dev, hkv = self.device, self.hkv
+        _expect_rows("k", k, hkv, None, dev)
+        T = k.shape[0]
+        _expect_rows("v", v, hkv, T, dev)
+        nseq, max_pages = self._batch(T, table, kv_len, cu)
+        hq, rot = hkv, 0
+        if q is not None:
+            if not isinstance(q, torch.Tensor) or q.dim() != 3:
+                raise NsaSelError("q must be bfloat16 [tokens, hq, 128]")
+            hq = q.shape[1]
+            _expect_rows("q", q, hq, T, dev)
+            if q_out is None:
+                q_out = torch.empty((T, hq, _D), dtype=_BF16, device=dev)
+            else:
+                expect_tensor("q_out", q_out, _BF16, (T, hq, _D), dev)
+        elif q_out is not None:
+            raise NsaSelError("q_out without q")
+        if k_out is not None:
+            expect_tensor("k_out", k_out, _BF16, (T, hkv, _D), dev)
+        elif rotated_k:
+            k_out = torch.empty((T, hkv, _D), dtype=_BF16, device=dev)
+        if inv_freq is not None:
+            expect_tensor("inv_freq", inv_freq, _F64, (inv_freq.numel(),), dev)
+            rot = 2 * inv_freq.numel()
+        kp, vp, ks, vs = self._pointers
+        shape = CacheShape(T, nseq, hq, hkv, _D, self._dtype, self.page, self.n_pages, max_pages, 64, 0, 0, 0.0)
+        _launch(lib().nsa_sel_cache_append, "nsa_sel_cache_append", dev, C.byref(shape), _ptr(q), 0 if q is None else _token_stride(q),
+                _ptr(k), _token_stride(k), _ptr(v), _token_stride(v), _ptr(cu), _ptr(kv_len), _ptr(table), _ptr(inv_freq), rot,
+                int(interleaved), kp, vp, ks, vs, _ptr(q_out), _ptr(k_out))
+        return q_out, k_out
+
+    def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
+        """Bytes that attention() of such a call needs as `ws`."""
+        return self._ws_bytes(CacheShape(tokens, nseq, hq, self.hkv, _D, self._dtype, self.page, self.n_pages, max_pages, block, topk, window, 0.0))
+
+    @staticmethod
+    def _ws_bytes(shape) -> int:
+        n = C.c_size_t()
+        _check(lib().nsa_sel_cache_workspace_bytes(C.byref(shape), C.byref(n)), "nsa_sel_cache_workspace_bytes")
+        return n.value
+
+    def attention(self, q: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
+                  idx: Optional[torch.Tensor] = None, block: int = 64, window: int = 0, scale: float = 0.0,
+                  gate: Optional[torch.Tensor] = None, o_acc: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+        """(O, LSE) of the new tokens' queries (bfloat16 [tokens, hq, 128], rotated) over the cache, their own keys included: over the
+        blocks of `idx` (int32 [tokens, hkv, topk]; select_blocks with kv_len gives it), over the last `window` places, over both, or over
+        every key.  With gate (float32 [tokens, hq]) O is o_acc + gate * O, the sum over a layer's branches.
+
+        out / lse take the results (out may be o_acc); rows of tokens that belong to no sequence are left as they are there, and
+        uninitialised otherwise.  ws, of workspace_bytes(), is for callers that may not allocate."""
+        dev = self.device
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise NsaSelError("q must be bfloat16 [tokens, hq, 128]")
+        T, hq = q.shape[0], q.shape[1]
+        rows = (T, hq, _D)
+        expect_tensor("q", q, _BF16, rows, dev)
+        nseq, max_pages = self._batch(T, table, kv_len, cu)
+        topk = 0
+        if idx is not None:
+            if not isinstance(idx, torch.Tensor) or idx.dim() != 3:
+                raise NsaSelError("idx must be int32 [tokens, hkv, topk]")
+            topk = idx.shape[2]
+            if topk < 1:
+                raise NsaSelError("idx must have a column")
+            expect_tensor("idx", idx, _I32, (T, self.hkv, topk), dev)
+        if gate is not None:
+            expect_tensor("gate", gate, _F32, (T, hq), dev)
+            if o_acc is not None:
+                expect_tensor("o_acc", o_acc, _BF16, rows, dev)
+        elif o_acc is not None:
+            raise NsaSelError("o_acc without gate")
+        if out is None:
+            out = torch.empty(rows, dtype=_BF16, device=dev)
+        else:
+            expect_tensor("out", out, _BF16, rows, dev)
+        if lse is None:
+            lse = torch.empty((T, hq), dtype=_F32, device=dev)
+        else:
+            expect_tensor("lse", lse, _F32, (T, hq), dev)
+        shape = CacheShape(T, nseq, hq, self.hkv, _D, self._dtype, self.page, self.n_pages, max_pages, block, topk, window, scale)
+        need = self._ws_bytes(shape)
+        if ws is not None:
+            expect_workspace("ws", ws, need, dev)
+        elif need:
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        kp, vp, ks, vs = self._pointers
+        _launch(lib().nsa_sel_cache_attention, "nsa_sel_cache_attention", dev, C.byref(shape), _ptr(q), _ptr(idx), _ptr(cu), _ptr(kv_len),
+                _ptr(table), kp, vp, ks, vs, _ptr(gate), _ptr(o_acc), _ptr(out), _ptr(lse), _ptr(ws), 0 if ws is None else need)
+        return out, lse

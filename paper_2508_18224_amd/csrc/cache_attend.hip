@@ -1,0 +1,481 @@
+// Attention of a few new tokens over a paged cache (nsa_sel_cache_attention): of selected blocks, of a window, or of every key.
+//
+// One pass over the keys with the running maximum and sum of a softmax.  What bounds it is reading the keys and values, which nothing else
+// reads: 4 g flops a byte in bf16 and twice that in 8 bits, far below what the matrix cores need to be busy.  So the products may waste
+// most of their columns (g of 16 are in use for a token), and everything serves having bytes in flight: a wavefront takes pieces of 32
+// keys by itself, K straight into the registers that the product reads, V through registers into a tile of its own in LDS, and the next
+// piece is requested as soon as the registers are free.  Four wavefronts, each with every fourth piece, join their sums in LDS; where
+// there are too few rows to fill the chip several workgroups share one, and a second kernel joins theirs.
+//
+// S^T = K Q^T by 16x16x32 products: a lane holds four consecutive keys of one column, and the keys of two 16-key tiles are eight
+// consecutive contraction steps of O^T += V^T P^T if V's rows are read in the same order.  Nothing is transposed but V, by the LDS read.
+//
+// e4m3 values become bf16 in registers, times their page's power of two, which bf16 holds exactly: the products are those of a bf16 cache.
+#include "cache.h"
+
+namespace nsa {
+namespace {
+
+constexpr int kWaves = kAttendWaves, kPiece = kAttendPiece, kTiles = kPiece / 16;
+constexpr int kVRow = kD * 2;                 // bytes of a row of V in LDS, its 16-byte chunks turned (row_turn)
+constexpr int kSumRow = kD * 4 + 16;          // bytes of a column's sums in LDS
+constexpr int kOwnLds = (16 * kSumRow + 2 * 16 * 4 + 255) & ~255;  // a wavefront's: its tile of V, and later its sums and their statistics
+constexpr int kAttendLds = kWaves * kOwnLds;
+static_assert(kPiece * kVRow <= kOwnLds, "the tile of a wavefront must fit");
+static_assert(kTiles == 2, "a piece is one contraction step of the PV product");
+
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A workgroup's share of the call: `nt` consecutive new tokens t0.. of sequence s, the first of them at `place`.
+struct Share {
+  int s, t0, nt, place, j, split;
+};
+
+// What a piece consists of: 16-key tiles, each in one page.
+struct Piece {
+  int key0;            // place of its first key
+  int64_t row[kTiles];   // of the pages' rows, its first
+  int rows[kTiles];      // that anything of the workgroup sees; 0 where there is no page
+  float ks[kTiles], vs[kTiles];
+};
+__device__ __forceinline__ float lane_float(float x, int l) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
+}
+
+template <bool kE4m3>
+struct Raw {  // a piece of K or V as it was read
+  u32x4 x[kTiles * (kE4m3 ? 2 : 4)];
+};
+
+// Buffer of a tile's rows; those that nothing sees read as zero.
+template <bool kE4m3>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const char* base, const Piece& P, int i) {
+  constexpr int kRow = kD * (kE4m3 ? 1 : 2);
+  return buffer_of(base + P.row[i] * kRow, (uint32_t)(P.rows[i] * kRow));
+}
+// K: lane (row lane & 15, quarter lane >> 4) takes the 16 bytes of each contraction step that the product wants of it.
+template <bool kE4m3>
+__device__ __forceinline__ void load_keys(const Cache& C, const Piece& P, int lane, Raw<kE4m3>& r) {
+  constexpr int kRow = kD * (kE4m3 ? 1 : 2), kN = kE4m3 ? 2 : 4;
+  const uint32_t off = (lane & 15) * kRow + (lane >> 4) * 16;
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    const __amdgpu_buffer_rsrc_t b = tile_buffer<kE4m3>(C.k, P, i);
+#pragma unroll
+    for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, off + 64 * s, 0, 0);
+  }
+}
+// V: 1 KB of consecutive rows a load.
+template <bool kE4m3>
+__device__ __forceinline__ void load_values(const Cache& C, const Piece& P, int lane, Raw<kE4m3>& r) {
+  constexpr int kN = kE4m3 ? 2 : 4;
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    const __amdgpu_buffer_rsrc_t b = tile_buffer<kE4m3>(C.v, P, i);
+#pragma unroll
+    for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, 1024 * s + lane * 16, 0, 0);
+  }
+}
+
+// Four e4m3 values times 2^e (the exponent of `scale`) as bf16.
+__device__ __forceinline__ uint2 four_bf16(uint32_t x, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+  return {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+}
+__device__ __forceinline__ u32x4 eight_bf16(uint32_t lo, uint32_t hi, float scale) {
+  const uint2 a = four_bf16(lo, scale), b = four_bf16(hi, scale);
+  return u32x4{a.x, a.y, b.x, b.y};
+}
+
+// kSelected: the blocks of idx, a token a workgroup.  kGroup: every key, and A.group tokens of a sequence a workgroup.  Neither: every key, a token.
+template <bool kE4m3, bool kSelected, bool kGroup>
+__global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Cache C, CacheAttend A) {
+  extern __shared__ __align__(256) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, qg = lane >> 4;
+  Share W;
+  {
+    int b = (int)blockIdx.x;
+    W.split = b % A.splits;
+    b /= A.splits;
+    W.j = b % C.hkv;
+    b /= C.hkv;
+    if constexpr (!kGroup) {
+      const TokenPlace p = token_place(C, b);
+      W.s = p.s;
+      W.place = p.place;
+      W.t0 = b;
+      W.nt = 1;
+    } else {
+      // groups of A.group tokens: a sequence's start at floor(cu / group) + s, room for all of them without a scan over the batch
+      auto base = [&](int s) { return (int64_t)(C.cu[s] / A.group) + s; };
+      W.s = find_sequence(C.nseq, b, base);
+      if (W.s >= 0) {
+        const int c0 = C.cu[W.s], n = C.cu[W.s + 1] - c0, i0 = (b - (int)base(W.s)) * A.group;
+        W.t0 = c0 + i0;
+        W.nt = min(min(A.group, n - i0), C.T - W.t0);
+        W.place = C.kv_len[W.s] - n + i0;
+        if (W.nt <= 0 || W.t0 < 0) W.s = -1;
+      }
+    }
+    if (W.s < 0) return;  // the whole workgroup
+    // the same in every lane, and said so: the buffers below are scalar
+    W.s = __builtin_amdgcn_readfirstlane(W.s);
+    W.t0 = __builtin_amdgcn_readfirstlane(W.t0);
+    W.nt = __builtin_amdgcn_readfirstlane(W.nt);
+    W.place = __builtin_amdgcn_readfirstlane(W.place);
+    W.j = __builtin_amdgcn_readfirstlane(W.j);
+  }
+  const int limit = C.max_pages << C.page_log2;  // places that the table can name
+  // this lane's column: token tt of the group, head hh; it sees the places [c_lo, c_hi)
+  const int tt = kGroup ? col / C.g : 0, hh = col - tt * C.g, cols = W.nt * C.g;
+  const bool used = col < cols;
+  const int c_hi = used ? min(W.place + tt + 1, limit) : 0, c_lo = A.window > 0 && used ? max(W.place + tt + 1 - A.window, 0) : 0;
+  // what any column sees, and what all of them see
+  const int lo = A.window > 0 ? max(W.place + 1 - A.window, 0) : 0, hi = min(W.place + W.nt, limit);
+  const int all_lo = A.window > 0 ? max(W.place + W.nt - A.window, 0) : 0, all_hi = min(W.place + 1, limit);
+
+  bf16x8 qf[4];
+  {
+    const bf16_t* src = (const bf16_t*)A.Q + ((int64_t)(W.t0 + (used ? tt : 0)) * C.hq + W.j * C.g + (used ? hh : 0)) * kD;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      // e4m3: the 16 bytes a lane reads are two contraction steps
+      const int d = kE4m3 ? 64 * (s >> 1) + 16 * qg + 8 * (s & 1) : 32 * s + 8 * qg;
+      u32x4 x = *reinterpret_cast<const u32x4*>(src + d);
+      if (!used) x = u32x4{0u, 0u, 0u, 0u};
+      qf[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+
+  // the pieces: of the kept blocks in their order, or all from lo to hi
+  int n_pieces, first_piece = 0, blocks = 0;
+  const int per_block = A.block / kPiece;
+  if constexpr (kSelected) {
+    const int my = lane < A.topk ? A.idx[((int64_t)W.t0 * C.hkv + W.j) * A.topk + lane] : -1;
+    const int64_t b0 = (int64_t)my * A.block;
+    const bool ok = my >= 0 && b0 < hi && b0 + A.block > lo;
+    const uint64_t okm = __builtin_amdgcn_ballot_w64(ok);
+    uint64_t keep = 0;
+    for (int m = 0; m < A.topk; ++m) {
+      if (!((okm >> m) & 1)) continue;
+      const int x = __builtin_amdgcn_readlane(my, m);
+      const uint64_t same = __builtin_amdgcn_ballot_w64(ok && my == x) & ((1ull << m) - 1ull);
+      if (same == 0) keep |= 1ull << m;
+    }
+    // lane i gets the i-th kept block
+    const int below = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(keep >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)keep, 0));
+    const int to = ((keep >> lane) & 1) ? below : 63 - (lane - below);
+    blocks = __builtin_amdgcn_ds_permute(to << 2, my);
+    n_pieces = __builtin_popcountll(keep) * per_block;
+  } else {
+    first_piece = lo / kPiece;
+    n_pieces = max((hi + kPiece - 1) / kPiece - first_piece, 0);
+  }
+
+  // pieces w, w + step, ...: their places, pages and scales, kAhead pieces at a time, piece lane / kTiles of these and its tile lane % kTiles
+  constexpr int kAhead = 64 / kTiles;
+  const int step = A.splits * kWaves, w0 = W.split * kWaves + wave;
+  const int mine = n_pieces > w0 ? (n_pieces - w0 + step - 1) / step : 0;
+  int key_of = 0, rows_of = 0;
+  int64_t row_of = 0;
+  float k_scale = 1.f, v_scale = 1.f;
+  auto look_up = [&](int i) __attribute__((always_inline)) {
+    const int p = w0 + (i + lane / kTiles) * step, pc = min(p, max(n_pieces - 1, 0));
+    if constexpr (kSelected) {
+      const int o = pc / per_block;
+      const int id = (int)lane_value((uint32_t)blocks, o);
+      key_of = id * A.block + (pc - o * per_block) * kPiece;
+    } else {
+      key_of = (first_piece + pc) * kPiece;
+    }
+    const int key = key_of + 16 * (lane % kTiles), page = p < n_pieces ? page_of(C, W.s, key) : -1;
+    rows_of = page < 0 ? 0 : min(max(hi - key, 0), 16);
+    const int64_t at = (int64_t)max(page, 0) * C.hkv + W.j;
+    row_of = (at << C.page_log2) + (key & ((1 << C.page_log2) - 1));
+    if constexpr (kE4m3) {
+      if (page >= 0) {
+        k_scale = C.ks[at];
+        v_scale = C.vs[at];
+      }
+    }
+  };
+  auto piece = [&](int i) __attribute__((always_inline)) {
+    Piece P;
+    const int l = (i % kAhead) * kTiles;
+    P.key0 = __builtin_amdgcn_readlane(key_of, l);
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      P.rows[x] = __builtin_amdgcn_readlane(rows_of, l + x);
+      P.row[x] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(row_of >> 32), l + x) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)row_of, l + x));
+      P.ks[x] = kE4m3 ? lane_float(k_scale, l + x) : 1.f;
+      P.vs[x] = kE4m3 ? lane_float(v_scale, l + x) : 1.f;
+    }
+    return P;
+  };
+
+  const float c2 = A.scale * 1.4426950408889634f;
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x4 oacc[8];
+#pragma unroll
+  for (int d = 0; d < 8; ++d) oacc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t v_lds = lds_address(smem) + wave * kOwnLds;
+  // V^T operand of channels 16 d ..: rows (col / 4) + 4 qg and those 16 on, columns 16 d + 4 (col % 4).  The tile lies at a multiple of 256
+  // bytes, so a chunk's place is flipped into the address; done anew for every piece, it takes no registers.
+  const int v_row = (col >> 2) + 4 * qg;
+  const uint32_t v_at = v_lds + v_row * kVRow + ((((col & 3) >> 1) ^ row_turn(v_row)) << 4) + 8 * (col & 1);
+  auto values = [&](uint32_t at, int d) __attribute__((always_inline)) {
+    const uint32_t a = at ^ (d << 5);
+    return __builtin_shufflevector(lds_read_tr_at(a), lds_read_tr_at(a + 16 * kVRow), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // where this lane's 16 bytes of a load go (e4m3: the first of two chunks): row lane / 16 of four (lane / 8 of eight), whose turn the
+  // later rows of the tile flip further
+  const int w_row = kE4m3 ? lane >> 3 : lane >> 4;
+  const uint32_t w_at = v_lds + w_row * kVRow + (((kE4m3 ? 2 * (lane & 7) : col) ^ row_turn(w_row)) << 4);
+  Raw<kE4m3> kr, vr;
+  Piece P;
+  if (mine > 0) {
+    look_up(0);
+    P = piece(0);
+    load_keys<kE4m3>(C, P, lane, kr);
+    load_values<kE4m3>(C, P, lane, vr);
+  }
+  for (int i = 0; i < mine; ++i) {
+    const Piece cur = P;
+    f32x4 sacc[kTiles];
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      sacc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        u32x4 a;
+        if constexpr (kE4m3) {
+          const u32x4 r = kr.x[2 * x + (s >> 1)];
+          a = (s & 1) ? eight_bf16(r[2], r[3], cur.ks[x]) : eight_bf16(r[0], r[1], cur.ks[x]);
+        } else {
+          a = kr.x[4 * x + s];
+        }
+        sacc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), qf[s], sacc[x], 0, 0, 0);
+      }
+    }
+    const bool more = i + 1 < mine;
+    if (more) {
+      if ((i + 1) % kAhead == 0) look_up(i + 1);
+      P = piece(i + 1);
+      load_keys<kE4m3>(C, P, lane, kr);
+    }
+    // scores of places that the column does not see become -inf
+    bool whole = cur.key0 >= all_lo && cur.key0 + kPiece <= all_hi;
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) whole = whole && cur.rows[x] > 0;
+    float m = -INFINITY;
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = cur.key0 + 16 * x + 4 * qg + e;
+          if (key < c_lo || key >= c_hi || cur.rows[x] == 0) sacc[x][e] = -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, sacc[x][e]);
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float m_new = fmaxf(m_run, m);
+    const float mc = m_new == -INFINITY ? 0.f : m_new * c2;
+    const float alpha = __builtin_amdgcn_exp2f(fmaf(m_run, c2, -mc));  // exp2(-inf) = 0 on the first piece with a score
+    m_run = m_new;
+    float l = 0.f;
+    bf16x8 pf;
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sacc[x][e], c2, -mc));
+        l += p;
+        pf[4 * x + e] = (bf16_t)p;
+      }
+    l_run = fmaf(l_run, alpha, l);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) oacc[d] *= alpha;
+    uint32_t va = v_at, wa = w_at;
+    asm volatile("" : "+v"(va), "+v"(wa));  // what derives from them is not kept from piece to piece
+    // V into this wavefront's tile; rows before anything that the group sees as zeros, whatever they hold
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      constexpr int kN = kE4m3 ? 2 : 4;
+#pragma unroll
+      for (int s = 0; s < kN; ++s) {
+        u32x4 r = vr.x[x * kN + s];
+        const int row = 16 * x + (kE4m3 ? 8 : 4) * s;
+        if (cur.key0 + row + w_row < lo) r = u32x4{0u, 0u, 0u, 0u};
+        const uint32_t at = (wa ^ (row_turn(row) << 4)) + row * kVRow;
+        if constexpr (kE4m3) {
+          lds_write_16(at, eight_bf16(r[0], r[1], cur.vs[x]));
+          lds_write_16(at ^ 16, eight_bf16(r[2], r[3], cur.vs[x]));
+        } else {
+          lds_write_16(at, r);
+        }
+      }
+    }
+    if (more) load_values<kE4m3>(C, P, lane, vr);
+    wave_sync();
+    if (!kGroup || (cur.key0 >= all_lo && cur.key0 + kPiece <= all_hi)) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values(va, d), pf, oacc[d], 0, 0, 0);
+    } else {
+      // Tokens of the group see different keys of the piece, and what one does not see may be an infinity or a NaN, which a
+      // probability of zero does not silence: one token at a time, the others' keys as zeros.
+      for (int k = 0; k < W.nt; ++k) {
+        const int k_hi = min(W.place + k + 1, limit) - cur.key0, k_lo = (A.window > 0 ? max(W.place + k + 1 - A.window, 0) : 0) - cur.key0;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          bf16x8 a = values(va, d);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int key = 16 * (e >> 2) + 4 * qg + (e & 3);
+            if (key < k_lo || key >= k_hi) a[e] = (bf16_t)0.f;
+          }
+          const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          if (tt == k) oacc[d] += add;
+        }
+      }
+    }
+    wave_sync();  // the tile is overwritten by the next piece
+  }
+  l_run += __shfl_xor(l_run, 16);
+  l_run += __shfl_xor(l_run, 32);
+
+  // join the four wavefronts
+  {
+    char* own = smem + wave * kOwnLds;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) *reinterpret_cast<f32x4*>(own + col * kSumRow + (16 * d + 4 * qg) * 4) = oacc[d];
+    if (qg == 0) {
+      reinterpret_cast<float*>(own + 16 * kSumRow)[col] = m_run;
+      reinterpret_cast<float*>(own + 16 * kSumRow)[16 + col] = l_run;
+    }
+  }
+  __syncthreads();
+  const int c = threadIdx.x >> 4, sub = threadIdx.x & 15;
+  if (c >= cols) return;
+  float top = -INFINITY, total = 0.f, o[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, reinterpret_cast<const float*>(smem + w * kOwnLds + 16 * kSumRow)[c]);
+  const float tc = top == -INFINITY ? 0.f : top * c2;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const char* from = smem + w * kOwnLds;
+    const float* ml = reinterpret_cast<const float*>(from + 16 * kSumRow);
+    const float f = __builtin_amdgcn_exp2f(fmaf(ml[c], c2, -tc));
+    total = fmaf(f, ml[16 + c], total);
+    const f32x4 a = *reinterpret_cast<const f32x4*>(from + c * kSumRow + 32 * sub), b = *reinterpret_cast<const f32x4*>(from + c * kSumRow + 32 * sub + 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[e] = fmaf(f, a[e], o[e]);
+      o[4 + e] = fmaf(f, b[e], o[4 + e]);
+    }
+  }
+  const int ct = kGroup ? c / C.g : 0;
+  const int64_t row = (int64_t)(W.t0 + ct) * C.hq + W.j * C.g + (c - ct * C.g);
+  if (A.splits > 1) {
+    float* dst = A.part + (row * A.splits + W.split) * kD + 8 * sub;
+    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0], o[1], o[2], o[3]};
+    *reinterpret_cast<f32x4*>(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
+    if (sub == 0) A.part_ml[row * A.splits + W.split] = float2{top, total};
+    return;
+  }
+  const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] *= inv;
+  if (A.gate) {
+    const float gate = A.gate[row];
+    u32x4 x = u32x4{0u, 0u, 0u, 0u};
+    if (A.o_acc) x = *reinterpret_cast<const u32x4*>((const bf16_t*)A.o_acc + row * kD + 8 * sub);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[2 * e] = fmaf(gate, o[2 * e], bf16_lo(x[e]));
+      o[2 * e + 1] = fmaf(gate, o[2 * e + 1], bf16_hi(x[e]));
+    }
+  }
+  u32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
+  *reinterpret_cast<u32x4*>((bf16_t*)A.O + row * kD + 8 * sub) = x;
+  if (sub == 0) A.LSE[row] = total > 0.f || total != total ? (tc + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+// The splits of a row: a wavefront a row, two channels a lane.
+__global__ void __launch_bounds__(256) k_cache_join(Cache C, CacheAttend A) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= (int64_t)C.T * C.hq) return;
+  const int lane = threadIdx.x & 63, t = (int)(row / C.hq);
+  if (C.cu && (t < C.cu[0] || t >= C.cu[C.nseq])) return;  // rows of no sequence are left as they were
+  const float c2 = A.scale * 1.4426950408889634f;
+  const float2* ml = A.part_ml + row * A.splits;
+  float top = -INFINITY;
+  for (int s = 0; s < A.splits; ++s) top = fmaxf(top, ml[s].x);
+  const float tc = top == -INFINITY ? 0.f : top * c2;
+  const f32x2* from = reinterpret_cast<const f32x2*>(A.part + row * A.splits * kD) + lane;
+  float total = 0.f;
+  f32x2 o = {0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < A.splits; ++s) {
+    const float2 x = ml[s];
+    const float f = __builtin_amdgcn_exp2f(fmaf(x.x, c2, -tc));
+    const f32x2 v = from[s * (kD / 2)];
+    total = fmaf(f, x.y, total);
+    o[0] = fmaf(f, v[0], o[0]);
+    o[1] = fmaf(f, v[1], o[1]);
+  }
+  const bool some = total > 0.f || total != total;
+  const float inv = some ? 1.f / total : 0.f;
+  o[0] *= inv;
+  o[1] *= inv;
+  if (A.gate) {
+    const float gate = A.gate[row];
+    const uint32_t x = A.o_acc ? reinterpret_cast<const uint32_t*>(A.o_acc)[row * (kD / 2) + lane] : 0u;
+    o[0] = fmaf(gate, o[0], bf16_lo(x));
+    o[1] = fmaf(gate, o[1], bf16_hi(x));
+  }
+  reinterpret_cast<uint32_t*>(A.O)[row * (kD / 2) + lane] = pack_bf16x2(o[0], o[1]);
+  if (lane == 0) A.LSE[row] = some ? (tc + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+}  // namespace
+
+hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, hipStream_t st) {
+  // workgroups: a token and head, or a group of tokens of a sequence and head, times the splits
+  const bool grouped = A.group > 1;
+  const int64_t groups = grouped ? C.T / A.group + C.nseq : C.T;
+  const int64_t grid = groups * C.hkv * A.splits;
+  static std::atomic<uint64_t> ready[6];
+  static constexpr decltype(&k_cache_attend<false, false, false>) kForms[6] = {
+      k_cache_attend<false, false, false>, k_cache_attend<true, false, false>, k_cache_attend<false, false, true>,
+      k_cache_attend<true, false, true>,   k_cache_attend<false, true, false>, k_cache_attend<true, true, false>};
+  const int form = (A.idx ? 4 : grouped ? 2 : 0) + (e4m3 ? 1 : 0);
+  const auto kern = kForms[form];
+  hipError_t e = allow_dynamic_lds((const void*)kern, kAttendLds, ready[form]);
+  if (e != hipSuccess) return e;
+  {
+    ProfScope ps(KID_CACHE_ATTEND, st);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * kWaves), kAttendLds, st, C, A);
+  }
+  e = hipGetLastError();
+  if (e != hipSuccess || A.splits == 1) return e;
+  ProfScope ps(KID_CACHE_JOIN, st);
+  hipLaunchKernelGGL(k_cache_join, dim3((unsigned)(((int64_t)C.T * C.hq + 3) / 4)), dim3(256), 0, st, C, A);
+  return hipGetLastError();
+}
+
+}  // namespace nsa

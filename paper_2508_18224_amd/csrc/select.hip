@@ -6,7 +6,7 @@
 // other: ~530 instructions per row.  Rows where too many scores agree in the bound's bits fall back to the general method
 // (select_by_rounds): one pick per round, each round two wave-wide reductions.  Each visible score is read from
 // HBM once, with 16-byte loads when the rows are 16-byte aligned.
-#include "common.h"
+#include "cache.h"
 
 namespace nsa {
 namespace {
@@ -296,10 +296,11 @@ __device__ __forceinline__ bool select_by_threshold(const RowInfo& R, int lane, 
 
 }  // namespace
 
-template <bool kVec, bool kMany>
+// kCached: the rows are new tokens of cached sequences, whose places come from kv_len (cu may be null: one token a sequence).
+template <bool kVec, bool kMany, bool kCached>
 __global__ void __launch_bounds__(64 * kSelWaves)
-k_select_blocks(const float* __restrict__ scores, int64_t stride, const int32_t* __restrict__ cu, int T, int nseq,
-                int hkv, int bk, int topk, int causal, int n_sink, int n_local, int32_t* __restrict__ idx) {
+k_select_blocks(const float* __restrict__ scores, int64_t stride, const int32_t* __restrict__ cu, const int32_t* __restrict__ kv_len, int T,
+                int nseq, int hkv, int bk, int topk, int causal, int n_sink, int n_local, int32_t* __restrict__ idx) {
   // per wavefront: the survivor list of the fast method, or the chunk picks of the general one
   __shared__ Survivor lds[kSelWaves][kMaxChunks * kMaxTopk];
   static_assert(kMaxSurv <= kMaxChunks * kMaxTopk, "survivor list must fit");
@@ -320,11 +321,30 @@ k_select_blocks(const float* __restrict__ scores, int64_t stride, const int32_t*
     if constexpr (kMany) asm volatile("" : "+v"(lane));  // what derives from it is not kept in registers from row to row
     if (t != t_known) {
       t_known = t;
-      int s, c0, c1;
-      seq_bounds(cu, nseq, T, t, s, c0, c1);
-      const int cur = (t - c0) / bk;
-      const int b_s = (c1 - c0 + bk - 1) / bk;
-      R.b_vis = causal ? (cur + 1 < b_s ? cur + 1 : b_s) : b_s;
+      int cur;
+      if constexpr (kCached) {
+        Cache C;
+        C.cu = cu;
+        C.kv_len = kv_len;
+        C.nseq = nseq;
+        const TokenPlace p = token_place(C, t);
+        if (p.s < 0) {                       // a token of no sequence: its row is left as it was
+          t_known = -1;
+          if (++j == hkv) {
+            j = 0;
+            ++t;
+          }
+          continue;
+        }
+        cur = p.place < 0 ? -1 : p.place / bk;
+        R.b_vis = cur + 1;
+      } else {
+        int s, c0, c1;
+        seq_bounds(cu, nseq, T, t, s, c0, c1);
+        cur = (t - c0) / bk;
+        const int b_s = (c1 - c0 + bk - 1) / bk;
+        R.b_vis = causal ? (cur + 1 < b_s ? cur + 1 : b_s) : b_s;
+      }
       if ((int64_t)R.b_vis > stride) R.b_vis = (int)stride;   // never read past a row, whatever cu says
       // forced blocks: sinks 0 .. ns-1, then cur - r0, cur - r0 - 1, ... (nl of them, all >= ns and < b_vis)
       R.ns = n_sink < R.b_vis ? n_sink : R.b_vis;
@@ -361,31 +381,53 @@ k_select_blocks(const float* __restrict__ scores, int64_t stride, const int32_t*
 
 using namespace nsa;
 
+namespace nsa {
+namespace {
+// kv_len null: rows of a training batch
+int launch_select(const float* scores, int64_t score_stride, const int32_t* cu, const int32_t* kv_len, int T, int nseq, int hkv, int block,
+                  int topk, bool causal, int n_sink, int n_local, int32_t* idx, hipStream_t st) {
+  if (n_sink < 0 || n_local < 0) return NSA_SEL_EINVAL;
+  if (block != kBlock && block != 2 * kBlock) return NSA_SEL_EUNSUPPORTED;
+  if (topk < 1 || topk > kMaxTopk) return NSA_SEL_EUNSUPPORTED;
+  if (!scores) score_stride = (int64_t)kMaxChunks * kChunkBlocks;   // no rows to stay inside
+  if (score_stride < 1 || score_stride > (int64_t)kMaxChunks * kChunkBlocks) return NSA_SEL_EUNSUPPORTED;
+  if (!idx || ((uintptr_t)scores & 3) || ((uintptr_t)idx & 3)) return NSA_SEL_EINVAL;   // scores may be NULL
+  if (!cu && nseq != (kv_len ? T : 1)) return NSA_SEL_EINVAL;
+  const int64_t rows = (int64_t)T * hkv;
+  if (rows == 0) return NSA_SEL_OK;
+  if (rows * topk >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
+  const bool many = !kv_len && eight_rows(rows, hkv);
+  const int64_t per = many ? kSelRows : 1;
+  const int64_t grid = (rows + kSelWaves * per - 1) / (kSelWaves * per);
+  if (grid >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
+  ProfScope prof(KID_SELECT_BLOCKS, st);
+  const bool vec = (score_stride & 3) == 0 && ((uintptr_t)scores & 15) == 0;
+  auto kern = kv_len ? (vec ? k_select_blocks<true, false, true> : k_select_blocks<false, false, true>)
+              : many ? (vec ? k_select_blocks<true, true, false> : k_select_blocks<false, true, false>)
+                     : (vec ? k_select_blocks<true, false, false> : k_select_blocks<false, false, false>);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * kSelWaves), 0, st, scores, score_stride, cu, kv_len, T, nseq, hkv, block, topk,
+                     causal ? 1 : 0, n_sink, n_local, idx);
+  return hipGetLastError() == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP;
+}
+}  // namespace
+}  // namespace nsa
+
 extern "C" int nsa_sel_select_blocks(const nsa_sel_shape* shape, const float* scores, int64_t score_stride,
                                      const int32_t* cu_seqlens, int32_t n_sink, int32_t n_local, int32_t* idx,
                                      void* stream) {
   if (!shape) return NSA_SEL_EINVAL;
-  if (shape->total_tokens < 0 || shape->nseq < 1 || shape->hkv < 1 || n_sink < 0 || n_local < 0) return NSA_SEL_EINVAL;
-  if (shape->block != kBlock && shape->block != 2 * kBlock) return NSA_SEL_EUNSUPPORTED;
-  if (shape->topk < 1 || shape->topk > kMaxTopk) return NSA_SEL_EUNSUPPORTED;
-  if (!scores) score_stride = (int64_t)kMaxChunks * kChunkBlocks;   // no rows to stay inside
-  if (score_stride < 1 || score_stride > (int64_t)kMaxChunks * kChunkBlocks) return NSA_SEL_EUNSUPPORTED;
-  if (!idx || ((uintptr_t)scores & 3) || ((uintptr_t)idx & 3)) return NSA_SEL_EINVAL;   // scores may be NULL
-  if (!cu_seqlens && shape->nseq != 1) return NSA_SEL_EINVAL;
-  const int64_t rows = (int64_t)shape->total_tokens * shape->hkv;
-  if (rows == 0) return NSA_SEL_OK;
-  if (rows * shape->topk >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
-  const bool many = eight_rows(rows, shape->hkv);
-  const int64_t per = many ? kSelRows : 1;
-  const int64_t grid = (rows + kSelWaves * per - 1) / (kSelWaves * per);
-  if (grid >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
-  hipStream_t st = (hipStream_t)stream;
-  ProfScope prof(KID_SELECT_BLOCKS, st);
-  const bool vec = (score_stride & 3) == 0 && ((uintptr_t)scores & 15) == 0;
-  auto kern = many ? (vec ? k_select_blocks<true, true> : k_select_blocks<false, true>)
-                   : (vec ? k_select_blocks<true, false> : k_select_blocks<false, false>);
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * kSelWaves), 0, st, scores, score_stride, cu_seqlens,
-                     shape->total_tokens, shape->nseq, shape->hkv, shape->block, shape->topk, shape->causal ? 1 : 0,
-                     (int)n_sink, (int)n_local, idx);
-  return hipGetLastError() == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP;
+  if (shape->total_tokens < 0 || shape->nseq < 1 || shape->hkv < 1) return NSA_SEL_EINVAL;
+  return launch_select(scores, score_stride, cu_seqlens, nullptr, shape->total_tokens, shape->nseq, shape->hkv, shape->block,
+                       shape->topk, shape->causal != 0, n_sink, n_local, idx, (hipStream_t)stream);
+}
+
+extern "C" int nsa_sel_select_blocks_cached(const nsa_sel_cache_shape* shape, const float* scores, int64_t score_stride,
+                                            const int32_t* cu_seqlens, const int32_t* kv_len, int32_t n_sink,
+                                            int32_t n_local, int32_t* idx, void* stream) {
+  if (!shape) return NSA_SEL_EINVAL;
+  if (shape->n_tokens < 0 || shape->nseq < 0 || (shape->nseq == 0 && shape->n_tokens > 0) || shape->hkv < 1) return NSA_SEL_EINVAL;
+  if (shape->nseq > (1 << 24)) return NSA_SEL_EUNSUPPORTED;
+  if (shape->n_tokens > 0 && (!kv_len || ((uintptr_t)kv_len & 3) || ((uintptr_t)cu_seqlens & 3))) return NSA_SEL_EINVAL;
+  return launch_select(scores, score_stride, cu_seqlens, kv_len, shape->n_tokens, shape->nseq, shape->hkv, shape->block, shape->topk,
+                       true, n_sink, n_local, idx, (hipStream_t)stream);
 }
