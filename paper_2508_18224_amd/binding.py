@@ -85,7 +85,7 @@ def _launch(fn, what: str, dev: torch.device, *args):
     """fn(*args, current stream of dev) with dev current; every argument has been checked."""
     if dev.type != "cuda":
         raise NsaSelError("tensors must be contiguous device tensors")
-    if torch.cuda.current_device() == dev.index:
+    if torch._C._cuda_getDevice() == dev.index:  # (a tensor of the device exists, so the runtime is up)
         rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
     else:
         with torch.cuda.device(dev):

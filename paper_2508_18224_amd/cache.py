@@ -13,24 +13,31 @@ _BF16, _F32, _I32, _F64 = torch.bfloat16, torch.float32, torch.int32, torch.floa
 _D = 128
 
 
-def _expect_rows(name: str, t, heads: int, tokens: Optional[int], device) -> None:
-    """bf16 [tokens, heads, 128] whose tokens may lie apart (a slice of one projection) but whose heads may not."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not _BF16 or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != _D:
-        raise NsaSelError(f"{name} must be bfloat16 [tokens, {heads}, {_D}]")
-    if tokens is not None and t.shape[0] != tokens:
-        raise NsaSelError(f"{name} must have {tokens} tokens, got {t.shape[0]}")
+def _rows(name: str, t, shape, device) -> int:
+    """Values between the tokens of a bf16 [tokens, heads, 128] tensor.  They may lie apart (a slice of one projection), its heads may not."""
+    if not isinstance(t, torch.Tensor):
+        raise NsaSelError(f"{name} must be a torch.Tensor")
+    if t.dtype is not _BF16 or t.shape != shape:
+        raise NsaSelError(f"{name} must be bfloat16 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if t.device != device:
         raise NsaSelError(f"{name} must live on {device}, got {t.device}")
-    if t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != _D)):
-        raise NsaSelError(f"the heads of a token of {name} must be contiguous")
-    if t.shape[0] > 1 and (t.stride(0) < heads * _D or t.stride(0) % 8):
-        raise NsaSelError(f"the tokens of {name} must be a multiple of 8 values apart, and not overlap")
-    if t.shape[0] > 0 and t.data_ptr() % 16:
+    tokens, heads, _ = shape
+    if t.data_ptr() & 15:
         raise NsaSelError(f"{name} must be 16-byte aligned")
+    if t.is_contiguous():
+        return heads * _D
+    each, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != _D):
+        raise NsaSelError(f"the heads of a token of {name} must be contiguous")
+    if tokens > 1 and (each < heads * _D or each & 7):
+        raise NsaSelError(f"the tokens of {name} must be a multiple of 8 values apart, and not overlap")
+    return each if tokens > 1 else heads * _D
 
 
-def _token_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * _D
+def _dims(name: str, t, n: int):
+    if not isinstance(t, torch.Tensor) or t.dim() != n:
+        raise NsaSelError(f"{name} must be a torch.Tensor of {n} dimensions")
+    return t.shape
 
 
 class PagedCache:
@@ -89,10 +96,8 @@ class PagedCache:
     def _batch(self, tokens: int, table, kv_len, cu) -> Tuple[int, int]:
         """(sequences, columns of table) after the checks that all calls share."""
         dev = self.device
-        if not isinstance(table, torch.Tensor) or table.dim() != 2:
-            raise NsaSelError("table must be int32 [sequences, max_pages]")
-        nseq, max_pages = table.shape
-        expect_tensor("table", table, _I32, (nseq, max_pages), dev)
+        nseq, max_pages = _dims("table", table, 2)
+        expect_tensor("table", table, _I32, table.shape, dev)
         expect_tensor("kv_len", kv_len, _I32, (nseq,), dev)
         if cu is not None:
             expect_tensor("cu_seqlens", cu, _I32, (nseq + 1,), dev)
@@ -111,20 +116,18 @@ class PagedCache:
         attention.  q_out / k_out take the results (they may be q / k themselves if those are contiguous); rows of tokens that belong to no
         sequence are left as they are there, and uninitialised otherwise."""
         dev, hkv = self.device, self.hkv
-        _expect_rows("k", k, hkv, None, dev)
-        T = k.shape[0]
-        _expect_rows("v", v, hkv, T, dev)
+        T = _dims("k", k, 3)[0]
+        k_stride, v_stride = _rows("k", k, (T, hkv, _D), dev), _rows("v", v, (T, hkv, _D), dev)
         nseq, max_pages = self._batch(T, table, kv_len, cu)
-        hq, rot = hkv, 0
+        hq, rot, q_stride, q_ptr = hkv, 0, 0, None
         if q is not None:
-            if not isinstance(q, torch.Tensor) or q.dim() != 3:
-                raise NsaSelError("q must be bfloat16 [tokens, hq, 128]")
-            hq = q.shape[1]
-            _expect_rows("q", q, hq, T, dev)
+            hq = _dims("q", q, 3)[1]
+            rows = (T, hq, _D)
+            q_stride, q_ptr = _rows("q", q, rows, dev), q.data_ptr()
             if q_out is None:
-                q_out = torch.empty((T, hq, _D), dtype=_BF16, device=dev)
+                q_out = torch.empty(rows, dtype=_BF16, device=dev)
             else:
-                expect_tensor("q_out", q_out, _BF16, (T, hq, _D), dev)
+                expect_tensor("q_out", q_out, _BF16, rows, dev)
         elif q_out is not None:
             raise NsaSelError("q_out without q")
         if k_out is not None:
@@ -132,13 +135,13 @@ class PagedCache:
         elif rotated_k:
             k_out = torch.empty((T, hkv, _D), dtype=_BF16, device=dev)
         if inv_freq is not None:
-            expect_tensor("inv_freq", inv_freq, _F64, (inv_freq.numel(),), dev)
-            rot = 2 * inv_freq.numel()
-        kp, vp, ks, vs = self._pointers
+            pairs = _dims("inv_freq", inv_freq, 1)[0]
+            expect_tensor("inv_freq", inv_freq, _F64, (pairs,), dev)
+            rot = 2 * pairs
         shape = CacheShape(T, nseq, hq, hkv, _D, self._dtype, self.page, self.n_pages, max_pages, 64, 0, 0, 0.0)
-        _launch(lib().nsa_sel_cache_append, "nsa_sel_cache_append", dev, C.byref(shape), _ptr(q), 0 if q is None else _token_stride(q),
-                _ptr(k), _token_stride(k), _ptr(v), _token_stride(v), _ptr(cu), _ptr(kv_len), _ptr(table), _ptr(inv_freq), rot,
-                int(interleaved), kp, vp, ks, vs, _ptr(q_out), _ptr(k_out))
+        _launch(lib().nsa_sel_cache_append, "nsa_sel_cache_append", dev, C.byref(shape), q_ptr, q_stride, k.data_ptr(), k_stride,
+                v.data_ptr(), v_stride, _ptr(cu), kv_len.data_ptr(), table.data_ptr(), _ptr(inv_freq), rot, int(interleaved),
+                *self._pointers, _ptr(q_out), _ptr(k_out))
         return q_out, k_out
 
     def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
@@ -162,17 +165,13 @@ class PagedCache:
         out / lse take the results (out may be o_acc); rows of tokens that belong to no sequence are left as they are there, and
         uninitialised otherwise.  ws, of workspace_bytes(), is for callers that may not allocate."""
         dev = self.device
-        if not isinstance(q, torch.Tensor) or q.dim() != 3:
-            raise NsaSelError("q must be bfloat16 [tokens, hq, 128]")
-        T, hq = q.shape[0], q.shape[1]
+        T, hq, _ = _dims("q", q, 3)
         rows = (T, hq, _D)
         expect_tensor("q", q, _BF16, rows, dev)
         nseq, max_pages = self._batch(T, table, kv_len, cu)
         topk = 0
         if idx is not None:
-            if not isinstance(idx, torch.Tensor) or idx.dim() != 3:
-                raise NsaSelError("idx must be int32 [tokens, hkv, topk]")
-            topk = idx.shape[2]
+            topk = _dims("idx", idx, 3)[2]
             if topk < 1:
                 raise NsaSelError("idx must have a column")
             expect_tensor("idx", idx, _I32, (T, self.hkv, topk), dev)
@@ -196,7 +195,7 @@ class PagedCache:
             expect_workspace("ws", ws, need, dev)
         elif need:
             ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        kp, vp, ks, vs = self._pointers
-        _launch(lib().nsa_sel_cache_attention, "nsa_sel_cache_attention", dev, C.byref(shape), _ptr(q), _ptr(idx), _ptr(cu), _ptr(kv_len),
-                _ptr(table), kp, vp, ks, vs, _ptr(gate), _ptr(o_acc), _ptr(out), _ptr(lse), _ptr(ws), 0 if ws is None else need)
+        _launch(lib().nsa_sel_cache_attention, "nsa_sel_cache_attention", dev, C.byref(shape), q.data_ptr(), _ptr(idx), _ptr(cu),
+                kv_len.data_ptr(), table.data_ptr(), *self._pointers, _ptr(gate), _ptr(o_acc), out.data_ptr(), lse.data_ptr(), _ptr(ws),
+                0 if ws is None else need)
         return out, lse

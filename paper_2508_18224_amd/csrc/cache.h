@@ -5,7 +5,7 @@
 
 namespace nsa {
 
-constexpr int kAttendPiece = 32, kAttendWaves = 4;   // keys of a step of the attention; wavefronts of a workgroup, which share its pieces
+constexpr int kAttendPiece = 32;  // keys of a step of the attention
 constexpr int kScaleLeast = -100, kScaleMost = 119;  // exponents of a page's scale: both it and its reciprocal are normal numbers
 
 struct Cache {
@@ -32,9 +32,15 @@ struct CacheAttend {
   void* O;
   float* LSE;
   int32_t group;       // new tokens of a sequence that a workgroup takes together
-  int32_t splits;      // workgroups that share a row's keys
-  float* part;         // [T * hq, splits, 128] sums, then [T * hq, splits] pairs (maximum, sum); with splits > 1
-  float2* part_ml;
+  int32_t splits;      // workgroups that may share the pieces of a row of selected blocks, `chunk` each
+  int32_t chunk;
+  int32_t even;        // else 0, or the number of workgroups that share all rows' pieces evenly
+  bool streaming;      // keys and values come from memory and will not be read again soon
+  // parts of rows, where a workgroup may have less than a whole one (else rows is null): slot i has `cols` columns, one for every token and head of a row
+  float* part;         // [slots, cols, 128] sums
+  float2* part_ml;     // [slots, cols] (maximum, sum)
+  int4* rows;          // [T, hkv] first slot, second slot, number of parts, first token of the row
+  int32_t slots, cols, slot_step;
 };
 hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, hipStream_t st);
 

@@ -57,9 +57,12 @@ int check_cache_pointers(const nsa_sel_cache_shape* s, const void* k, const void
   return NSA_SEL_OK;
 }
 
-// How the attention is cut: new tokens a workgroup takes together, and workgroups that share a row's keys.
+// How the attention is cut (see launch_cache_attend).
 struct Cut {
-  int group, splits;
+  int group;           // new tokens of a sequence that a workgroup takes together
+  int splits, chunk, even;
+  bool streaming;
+  int64_t slots;       // of parts; 0 where every row is one workgroup's
 };
 Cut cut_of(const nsa_sel_cache_shape* s) {
   Cut c;
@@ -68,19 +71,52 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   const int64_t most = 16 / g;
   c.group = s->topk > 0 ? 1 : (int)(each < most ? (each > 1 ? each : 1) : most);
   const int64_t rows = (s->n_tokens + c.group - 1) / c.group * (int64_t)s->hkv;
-  int64_t keys = (int64_t)s->max_pages * s->page;
-  if (s->topk > 0 && (int64_t)s->topk * s->block < keys) keys = (int64_t)s->topk * s->block;
-  if (s->window > 0 && (int64_t)s->window + c.group < keys) keys = (int64_t)s->window + c.group;
-  const int64_t pieces = (keys + kAttendPiece - 1) / kAttendPiece, target = s->topk > 0 || s->window > 0 ? 512 : 2048;
-  int64_t n = rows > 0 ? (target + rows - 1) / rows : 1;
-  const int64_t cap = (pieces + kAttendWaves - 1) / kAttendWaves;  // a piece a wavefront
-  if (n > cap) n = cap;
-  c.splits = (int)(n < 1 ? 1 : n > 128 ? 128 : n);
+  // upper bound of the pieces of a row (the kernel finds out how many there are, by the lengths and the kept blocks)
+  const int64_t limit = (int64_t)s->max_pages * s->page, window = s->window;
+  int64_t pieces = (limit + kAttendPiece - 1) / kAttendPiece;
+  if (s->topk > 0) {
+    int64_t blocks = (limit + s->block - 1) / s->block;
+    if (blocks > s->topk) blocks = s->topk;
+    if (window > 0 && blocks > window / s->block + 2) blocks = window / s->block + 2;
+    pieces = blocks * (s->block / kAttendPiece);
+  } else if (window > 0 && pieces > (window + c.group) / kAttendPiece + 2) {
+    pieces = (window + c.group) / kAttendPiece + 2;
+  }
+  if (pieces < 1) pieces = 1;
+  // Selected blocks: a row is one workgroup's, unless there are so few rows that those would read at the rate of a few compute units: then
+  // about 512 workgroups, of a piece a wavefront at least.  (16 blocks of 64, bf16, us, whole -> in parts of 4 pieces: 1 token x 8 heads 14.4 -> 9.8,
+  // 4 x 8 15.6 -> 12.4, 16 x 8 17.1 -> 21.8 (of 8: 19.2); 32 blocks of 128, 1 x 2 45 -> 11.2.)
+  int64_t chunk = (pieces * rows + 511) / 512;
+  if (chunk < 4) chunk = 4;
+  if (s->topk == 0 || 2 * chunk > pieces || (rows > 64 && pieces <= 64)) chunk = pieces;
+  // Every key: rows of up to 40 pieces, and many rows of a window, are a workgroup each; longer ones are cut evenly (see k_cache_attend_even).
+  // (8 heads, us, whole -> even: 16 sequences of 1024 14.9 -> 19.1, one of 2048 22 -> 10.2, a window of 512 x 128 sequences 12.3 -> 41, of 4096 x 64 170
+  // either way.)
+  const bool even = s->topk == 0 && pieces > 40 && s->nseq <= 4096 && !(window > 0 && rows >= 512);
+  // Non-temporal loads where the keys and values are more than the 256 MB of the memory-side cache keep from one call to the next, and not for
+  // new tokens of one sequence, which share blocks.  (16 blocks of 64, us, plain -> non-temporal: 256 tokens x 8 heads bf16, 1.05 GB, 188 -> 169; 32 x 8, 131 MB, 29.2
+  // -> 26.0; 16 x 8, 66 MB, 17.1 -> 22.9; drafts of one to eight tokens, 524 MB read of half as much, 79 -> 94.)
+  const bool streaming = rows * pieces * kAttendPiece * kD * (s->dtype == NSA_SEL_CACHE_E4M3 ? 2 : 4) > (96ll << 20) && s->n_tokens == s->nseq;
+  if (chunk > pieces) chunk = pieces;
+  c.chunk = (int)chunk;
+  c.splits = (int)((pieces + chunk - 1) / chunk);
+  c.even = even ? 512 : 0;
+  if (c.even && rows > (((int64_t)1 << 31) - 1) / pieces * c.even) c.even = 0;  // a share is a 32-bit number
+  c.streaming = streaming;
+  c.slots = c.even ? 2 * (int64_t)c.even : c.splits > 1 ? rows * c.splits : 0;
   return c;
 }
-size_t part_bytes(const nsa_sel_cache_shape* s, const Cut& c) { return (size_t)s->n_tokens * s->hq * c.splits * kD * 4; }
-size_t cache_ws_bytes(const nsa_sel_cache_shape* s, const Cut& c) {
-  return c.splits == 1 ? 0 : part_bytes(s, c) + (size_t)s->n_tokens * s->hq * c.splits * 8;
+struct CacheWs {
+  size_t ml, rows, total;  // offsets; the sums come first
+};
+CacheWs cache_ws(const nsa_sel_cache_shape* s, const Cut& c) {
+  CacheWs w = {0, 0, 0};
+  if (c.slots == 0) return w;
+  const size_t cols = (size_t)c.slots * c.group * (s->hq / s->hkv);
+  w.ml = cols * kD * 4;
+  w.rows = (w.ml + cols * 8 + 15) & ~(size_t)15;
+  w.total = w.rows + (size_t)s->n_tokens * s->hkv * 16;
+  return w;
 }
 
 }  // namespace
@@ -117,7 +153,7 @@ int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_
 int nsa_sel_cache_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes) {
   int rc = check_cache_shape(shape, true);
   if (rc) return rc;
-  if (bytes) *bytes = cache_ws_bytes(shape, cut_of(shape));
+  if (bytes) *bytes = cache_ws(shape, cut_of(shape)).total;
   return NSA_SEL_OK;
 }
 
@@ -133,11 +169,11 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
   if (!tensor(Q) || !tensor(O) || !ints(LSE) || !tensor(O_acc, true) || !ints(gate, true)) return NSA_SEL_EINVAL;
   if ((shape->topk > 0) != (idx != nullptr) || !ints(idx, true) || (O_acc && !gate) || O == Q) return NSA_SEL_EINVAL;
   const Cut c = cut_of(shape);
-  const size_t need = cache_ws_bytes(shape, c);
-  if (need > 0 && !tensor(ws)) return NSA_SEL_EINVAL;
-  if (ws_bytes < need) return NSA_SEL_EWORKSPACE;
+  const CacheWs w = cache_ws(shape, c);
+  if (w.total > 0 && !tensor(ws)) return NSA_SEL_EINVAL;
+  if (ws_bytes < w.total) return NSA_SEL_EWORKSPACE;
   const int64_t groups = c.group > 1 ? shape->n_tokens / c.group + (int64_t)shape->nseq : shape->n_tokens;
-  if (groups * shape->hkv * c.splits >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;  // workgroups
+  if (groups * shape->hkv * c.splits >= ((int64_t)1 << 31) || c.slots >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;  // workgroups
   CacheAttend A;
   A.Q = Q;
   A.idx = idx;
@@ -150,9 +186,16 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
   A.O = O;
   A.LSE = LSE;
   A.group = c.group;
-  A.splits = c.splits;
+  A.splits = c.even ? 1 : c.splits;
+  A.chunk = c.chunk;
+  A.even = c.even;
+  A.streaming = c.streaming;
   A.part = (float*)ws;
-  A.part_ml = (float2*)((char*)ws + part_bytes(shape, c));
+  A.part_ml = (float2*)((char*)ws + w.ml);
+  A.rows = c.slots > 0 ? (int4*)((char*)ws + w.rows) : nullptr;
+  A.cols = c.group * (shape->hq / shape->hkv);
+  A.slots = (int)c.slots;
+  A.slot_step = c.even ? 2 : 1;
   const Cache C = make_cache(shape, k_pages, v_pages, k_scale, v_scale, table, kv_len, cu_seqlens);
   return launch_cache_attend(C, shape->dtype == NSA_SEL_CACHE_E4M3, A, (hipStream_t)stream) == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP;
 }

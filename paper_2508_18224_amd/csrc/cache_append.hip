@@ -1,17 +1,20 @@
 // New keys and values into a paged cache, rotated by their places on the way, and the rotated queries beside them (nsa_sel_cache_append).
 //
 // Rotation by the place p: channels a, b of a pair i become  x_a cos(p f_i) - x_b sin(p f_i),  x_b cos(p f_i) + x_a sin(p f_i).  The angle
-// is taken in turns and in 64 bits, p f_i / 2 pi less its nearest whole number, so that a place of 2^20 loses nothing; its sine and cosine
-// are then those of a 32-bit angle in [-1/2, 1/2] turns.
+// is formed in 64 bits, in turns, less its nearest whole number, so that a place of 2^20 loses nothing.  What is stored as bf16 is then computed
+// in 32 bits.  Keys for 8 bits are computed in 64 and rounded once: near the border of two e4m3 values an error of 2^-24 in the value is
+// one of 2^-4 in what is stored.
 //
 // Memory bound: every value is read once and written once.  A row of 128 channels is 16 lanes with 16 bytes each; the partner of a
 // lane's channels is in another lane of the row, or in the lane itself where pairs lie side by side.
+#include <algorithm>
+
 #include "cache.h"
 
 namespace nsa {
 namespace {
 
-constexpr int kThreads = 256, kRowsAtOnce = kThreads / 16;
+constexpr int kRowThreads = 256, kMaxPairs = kD / 2;
 
 struct Rotation {
   const double* inv_freq;  // [rot / 2], radians per place
@@ -26,11 +29,28 @@ struct AppendArgs {
   Rotation R;
 };
 
-__device__ __forceinline__ float2 cos_sin(int place, double inv_freq) {
+// (cos, sin) of the angle place * inv_freq, as exact as that product: a multiple of a quarter turn off, then Taylor's series on
+// [-pi/4, pi/4], whose next terms are below 3e-14 and 1e-15.
+__device__ __forceinline__ double2 cos_sin(int place, double inv_freq) {
   const double turns = (double)place * inv_freq * 0.15915494309189533577;
-  float s, c;
-  sincospif((float)(2.0 * (turns - __builtin_rint(turns))), &s, &c);
-  return {c, s};
+  const double r = turns - __builtin_rint(turns), quarters = __builtin_rint(4.0 * r);
+  const double x = (r - 0.25 * quarters) * 6.283185307179586477, y = x * x;
+  double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
+  s = __builtin_fma(s, y, -1.0 / 39916800.0);
+  c = __builtin_fma(c, y, 1.0 / 479001600.0);
+  s = __builtin_fma(s, y, 1.0 / 362880.0);
+  c = __builtin_fma(c, y, -1.0 / 3628800.0);
+  s = __builtin_fma(s, y, -1.0 / 5040.0);
+  c = __builtin_fma(c, y, 1.0 / 40320.0);
+  s = __builtin_fma(s, y, 1.0 / 120.0);
+  c = __builtin_fma(c, y, -1.0 / 720.0);
+  s = __builtin_fma(s, y, -1.0 / 6.0);
+  c = __builtin_fma(c, y, 1.0 / 24.0);
+  s = __builtin_fma(s * y, x, x);
+  c = __builtin_fma(__builtin_fma(c, y, -0.5), y, 1.0);
+  const int q = (int)quarters;  // -2 .. 2
+  const double co = (q & 1) ? s : c, si = (q & 1) ? c : s;
+  return {((q + 1) & 2) ? -co : co, (q & 2) ? -si : si};
 }
 
 __device__ __forceinline__ void unpack(u32x4 x, float (&f)[8]) {
@@ -47,18 +67,33 @@ __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
   return r;
 }
 
+// 64-bit value as a float with the last bit set if that is not all of it: rounding that to fewer bits is rounding the value itself.
+__device__ __forceinline__ float to_odd(double y) {
+  const float f = (float)y;
+  const double rest = y - (double)f;
+  uint32_t u = __builtin_bit_cast(uint32_t, f);
+  if (rest != 0.0 && f != 0.f && (u & 1) == 0) u += (rest > 0.0) == (f > 0.f) ? 1 : -1;
+  return __builtin_bit_cast(float, u);
+}
+// u cos - v sin, in the precision of the angles
+__device__ __forceinline__ float turned(float u, float v, float2 t) { return u * t.x - v * t.y; }
+__device__ __forceinline__ float turned(float u, float v, double2 t) {
+  return to_odd(__builtin_fma((double)u, t.x, -((double)v * t.y)));
+}
+
 // The lane's 8 channels of a row after the rotation; cs: the row's (cos, sin) by pair.  All 16 lanes of the row take part.
-__device__ __forceinline__ void rotate(const Rotation& R, u32x4 x, const float2* cs, float (&f)[8]) {
+template <class Angle>
+__device__ __forceinline__ void rotate(const Rotation& R, u32x4 x, const Angle* cs, float (&f)[8]) {
   const int lane = threadIdx.x & 63, c = lane & 15, half = R.rot >> 4;  // 8-channel pieces of half the pairs
   unpack(x, f);
   if (R.interleaved) {
     if (8 * c < R.rot) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 t = cs[4 * c + i];
+        const Angle t = cs[4 * c + i];
         const float u = f[2 * i], v = f[2 * i + 1];
-        f[2 * i] = u * t.x - v * t.y;
-        f[2 * i + 1] = v * t.x + u * t.y;
+        f[2 * i] = turned(u, v, t);
+        f[2 * i + 1] = turned(v, -u, t);
       }
     }
     return;
@@ -71,29 +106,34 @@ __device__ __forceinline__ void rotate(const Rotation& R, u32x4 x, const float2*
   if (low || high) {
     float o[8];
     unpack(y, o);
-    const float2* t = cs + 8 * (low ? c : c - half);
+    const Angle* t = cs + 8 * (low ? c : c - half);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = f[i] * t[i].x + (low ? -o[i] : o[i]) * t[i].y;
+    for (int i = 0; i < 8; ++i) f[i] = turned(f[i], low ? o[i] : -o[i], t[i]);
   }
 }
 
 // (cos, sin) of `tokens` consecutive places for every pair, kMaxPairs apart, by the whole workgroup.
-constexpr int kMaxPairs = kD / 2;
-__device__ __forceinline__ void angles(const Rotation& R, int first, int tokens, float2* cs) {
+template <int kThreads, class Angle>
+__device__ __forceinline__ void angles(const Rotation& R, int first, int tokens, Angle* cs) {
   const int pairs = R.rot >> 1;
   for (int i = threadIdx.x; i < tokens * kMaxPairs; i += kThreads) {
     const int p = i & (kMaxPairs - 1);
-    if (p < pairs) cs[i] = cos_sin(first + i / kMaxPairs, R.inv_freq[p]);
+    if (p < pairs) {
+      const double2 t = cos_sin(first + i / kMaxPairs, R.inv_freq[p]);
+      cs[i].x = t.x;
+      cs[i].y = t.y;
+    }
   }
 }
 
 // ---- rows of tokens: queries, and the keys and values of a bf16 cache ------------------------------------------------------------------
 // A workgroup takes the rows of one token, or with blockIdx.y the part of them that is its own.
-template <bool kStore>
+template <int kThreads, bool kStore>
 __device__ __forceinline__ void token_rows(const Cache& C, const AppendArgs& A, int t, int part, int parts, float2* cs) {
   const TokenPlace P = token_place(C, t);
   if (P.s < 0 || P.place < 0) return;  // the same for the whole workgroup
-  angles(A.R, P.place, 1, cs);
+  constexpr int kRowsAtOnce = kThreads / 16;
+  angles<kThreads>(A.R, P.place, 1, cs);
   const int page = kStore ? page_of(C, P.s, P.place) : -1;
   __syncthreads();
   const int sub = threadIdx.x & 15, nq = A.Q ? C.hq : 0, rows = nq + (kStore ? 2 * C.hkv : 0);
@@ -121,9 +161,9 @@ __device__ __forceinline__ void token_rows(const Cache& C, const AppendArgs& A, 
   }
 }
 
-__global__ void __launch_bounds__(kThreads) k_cache_append_rows(Cache C, AppendArgs A) {
+__global__ void __launch_bounds__(kRowThreads) k_cache_append_rows(Cache C, AppendArgs A) {
   __shared__ float2 cs[kMaxPairs];
-  token_rows<true>(C, A, (int)blockIdx.x, (int)blockIdx.y, (int)gridDim.y, cs);
+  token_rows<kRowThreads, true>(C, A, (int)blockIdx.x, (int)blockIdx.y, (int)gridDim.y, cs);
 }
 
 // ---- pages in 8 bits -----------------------------------------------------------------------------------------------------------
@@ -158,9 +198,10 @@ __device__ __forceinline__ uint32_t rescale_e4m3(uint32_t x, float by) {
 
 // A workgroup takes the new tokens of one page for one KV head, of K or of V: their largest magnitude, the page's scale, and, where the
 // page held earlier tokens and the scale grew, those again.  Scales are powers of two so that this loses nothing but the last bits of
-// values that become subnormal, less than 2^-17 of the page's largest.  Up to 64 rows are kept in registers between the two
-// steps; larger pages are read and rotated twice.
-constexpr int kTileRows = 64, kSteps = kTileRows / kRowsAtOnce;
+// values that become subnormal, less than 2^-17 of the page's largest.  Between the two steps kSteps rows of each 16 lanes stay in
+// registers; a workgroup has as many threads as that takes for a whole page where pages fill up in the mean, else 256, and goes through the
+// rows twice where a page gets more.
+constexpr int kSteps = 4;
 struct PageUnit {
   int s, t0, first, rows, page;  // sequence, first new token and its place, new tokens in the page
 };
@@ -191,8 +232,9 @@ __device__ __forceinline__ PageUnit page_unit(const Cache& C, int u) {
   return U;
 }
 
-template <bool kKey>
-__device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, const PageUnit& U, int h, float2* cs, float* most) {
+template <int kThreads, bool kKey>
+__device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, const PageUnit& U, int h, double2* cs) {
+  constexpr int kRowsAtOnce = kThreads / 16, kTileRows = kSteps * kRowsAtOnce;
   const int sub = threadIdx.x & 15, rg = threadIdx.x >> 4;
   const bf16_t* src = kKey ? A.K : A.V;
   const int64_t stride = kKey ? A.k_stride : A.v_stride;
@@ -201,10 +243,6 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
   // the rows of tile `tile`, rotated; keys also leave as bf16 where that was asked for
   auto load = [&](int tile, bool write) __attribute__((always_inline)) {
     const int r0 = tile * kTileRows, rows = min(kTileRows, U.rows - r0);
-    if constexpr (kKey) {
-      __syncthreads();  // the last tile's angles have been read
-      angles(A.R, U.first + r0, rows, cs);
-    }
     u32x4 x[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
@@ -212,13 +250,15 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
       x[i] = u32x4{0u, 0u, 0u, 0u};
       if (r < rows) x[i] = *reinterpret_cast<const u32x4*>(src + (int64_t)(U.t0 + r0 + r) * stride + h * kD + 8 * sub);
     }
-    if constexpr (kKey) __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       if (i * kRowsAtOnce >= rows) break;  // the same for the whole workgroup
-      const int r = i * kRowsAtOnce + rg;
       if constexpr (kKey) {
-        rotate(A.R, x[i], cs + min(r, rows - 1) * kMaxPairs, f[i]);
+        const int r = i * kRowsAtOnce + rg, n = min(kRowsAtOnce, rows - i * kRowsAtOnce);
+        if (i > 0 || tile > 0 || !write) __syncthreads();  // what was there has been read
+        angles<kThreads>(A.R, U.first + r0 + i * kRowsAtOnce, n, cs);
+        __syncthreads();
+        rotate(A.R, x[i], cs + min(rg, n - 1) * kMaxPairs, f[i]);
         if (write && A.K_out && r < rows)
           *reinterpret_cast<u32x4*>(A.K_out + ((int64_t)(U.t0 + r0 + r) * C.hkv + h) * kD + 8 * sub) = pack(f[i]);
       } else {
@@ -233,19 +273,24 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       if (i * kRowsAtOnce >= rows) break;
+      if (i * kRowsAtOnce + rg < rows) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float a = __builtin_fabsf(f[i][e]);
-        amax = a < __builtin_inff() ? fmaxf(amax, a) : amax;
+        for (int e = 0; e < 8; ++e) {
+          const float a = __builtin_fabsf(f[i][e]);
+          amax = a < __builtin_inff() ? fmaxf(amax, a) : amax;
+        }
       }
     }
   }
   if (U.page < 0) return;  // the same for the whole workgroup
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
+  float* most = reinterpret_cast<float*>(cs);
+  __syncthreads();  // the angles have been read
   if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = amax;
   __syncthreads();
-  amax = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) amax = fmaxf(amax, most[w]);
   float* scale = (kKey ? C.ks : C.vs) + (int64_t)U.page * C.hkv + h;
   const int held = U.first & ((1 << C.page_log2) - 1);  // earlier tokens of the page
   int e = scale_exponent(amax), e_old = e;
@@ -279,13 +324,13 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
 }
 
 // Workgroups [0, units * hkv): pages of K; as many of V; then the query rows, a token each.
+template <int kThreads>
 __global__ void __launch_bounds__(kThreads) k_cache_append_e4m3(Cache C, AppendArgs A, int units) {
-  __shared__ float2 cs[kTileRows * kMaxPairs];
-  __shared__ float most[kThreads / 64];
+  __shared__ double2 cs[kThreads / 16 * kMaxPairs];
   const int n = units * C.hkv;
   int b = (int)blockIdx.x;
   if (b >= 2 * n) {
-    token_rows<false>(C, A, b - 2 * n, 0, 1, cs);
+    token_rows<kThreads, false>(C, A, b - 2 * n, 0, 1, reinterpret_cast<float2*>(cs));
     return;
   }
   const bool key = b < n;
@@ -293,8 +338,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_append_e4m3(Cache C, AppendA
   const int u = b / C.hkv, h = b - u * C.hkv;
   const PageUnit U = page_unit(C, u);
   if (U.rows <= 0 || U.t0 < 0) return;
-  if (key) page_rows<true>(C, A, U, h, cs, most);
-  else page_rows<false>(C, A, U, h, cs, most);
+  if (key) page_rows<kThreads, true>(C, A, U, h, cs);
+  else page_rows<kThreads, false>(C, A, U, h, cs);
 }
 
 }  // namespace
@@ -316,11 +361,14 @@ hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t
   A.R.interleaved = interleaved ? 1 : 0;
   ProfScope ps(KID_CACHE_APPEND, st);
   if (!e4m3) {
-    hipLaunchKernelGGL(k_cache_append_rows, dim3((unsigned)C.T, 1), dim3(kThreads), 0, st, C, A);
+    hipLaunchKernelGGL(k_cache_append_rows, dim3((unsigned)C.T, 1), dim3(kRowThreads), 0, st, C, A);
   } else {
     const int64_t units = C.cu ? ((int64_t)C.T >> C.page_log2) + 2 * (int64_t)C.nseq : C.nseq;
     const int64_t grid = 2 * units * C.hkv + (Q ? C.T : 0);
-    hipLaunchKernelGGL(k_cache_append_e4m3, dim3((unsigned)grid), dim3(kThreads), 0, st, C, A, (int)units);
+    const int rows = (int)std::min<int64_t>(1 << C.page_log2, C.T / std::max(C.nseq, 1));  // new tokens of a page, in the mean
+    const int threads = rows <= 64 ? 256 : rows <= 128 ? 512 : 1024;
+    const auto kern = threads == 256 ? k_cache_append_e4m3<256> : threads == 512 ? k_cache_append_e4m3<512> : k_cache_append_e4m3<1024>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(threads), 0, st, C, A, (int)units);
   }
   return hipGetLastError();
 }

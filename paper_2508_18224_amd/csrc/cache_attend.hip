@@ -4,7 +4,7 @@
 // reads: 4 g flops a byte in bf16 and twice that in 8 bits, far below what the matrix cores need to be busy.  So the products may waste
 // most of their columns (g of 16 are in use for a token), and everything serves having bytes in flight: a wavefront takes pieces of 32
 // keys by itself, K straight into the registers that the product reads, V through registers into a tile of its own in LDS, and the next
-// piece is requested as soon as the registers are free.  Four wavefronts, each with every fourth piece, join their sums in LDS; where
+// piece is requested as soon as the registers are free.  The wavefronts of a workgroup take pieces in turn and join their sums in LDS; where
 // there are too few rows to fill the chip several workgroups share one, and a second kernel joins theirs.
 //
 // S^T = K Q^T by 16x16x32 products: a lane holds four consecutive keys of one column, and the keys of two 16-key tiles are eight
@@ -16,7 +16,8 @@
 namespace nsa {
 namespace {
 
-constexpr int kWaves = kAttendWaves, kPiece = kAttendPiece, kTiles = kPiece / 16;
+constexpr int kWaves = 4;                    // of a workgroup
+constexpr int kPiece = kAttendPiece, kTiles = kPiece / 16;
 constexpr int kVRow = kD * 2;                 // bytes of a row of V in LDS, its 16-byte chunks turned (row_turn)
 constexpr int kSumRow = kD * 4 + 16;          // bytes of a column's sums in LDS
 constexpr int kOwnLds = (16 * kSumRow + 2 * 16 * 4 + 255) & ~255;  // a wavefront's: its tile of V, and later its sums and their statistics
@@ -30,9 +31,17 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// A workgroup's share of the call: `nt` consecutive new tokens t0.. of sequence s, the first of them at `place`.
-struct Share {
-  int s, t0, nt, place, j, split;
+// A row of the call: `nt` consecutive new tokens t0.. of sequence s, the first of them at `place`, and KV head j.
+struct Row {
+  int s, t0, nt, place, j;
+};
+// The part of a row's pieces that a workgroup takes: [begin, end).  If that is not all of them their sums go to a place of their own, `slot`, and
+// the part that begins with the first one leaves word of them for k_cache_join.
+struct Part {
+  int begin, end;
+  bool whole;
+  int slot;
+  int second, count;  // slots of the row's other parts: second, second + A.slot_step, ...; with the own one `count`
 };
 
 // What a piece consists of: 16-key tiles, each in one page.
@@ -58,7 +67,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const char* base, 
   return buffer_of(base + P.row[i] * kRow, (uint32_t)(P.rows[i] * kRow));
 }
 // K: lane (row lane & 15, quarter lane >> 4) takes the 16 bytes of each contraction step that the product wants of it.
-template <bool kE4m3>
+template <bool kE4m3, int kPolicy>
 __device__ __forceinline__ void load_keys(const Cache& C, const Piece& P, int lane, Raw<kE4m3>& r) {
   constexpr int kRow = kD * (kE4m3 ? 1 : 2), kN = kE4m3 ? 2 : 4;
   const uint32_t off = (lane & 15) * kRow + (lane >> 4) * 16;
@@ -66,18 +75,18 @@ __device__ __forceinline__ void load_keys(const Cache& C, const Piece& P, int la
   for (int i = 0; i < kTiles; ++i) {
     const __amdgpu_buffer_rsrc_t b = tile_buffer<kE4m3>(C.k, P, i);
 #pragma unroll
-    for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, off + 64 * s, 0, 0);
+    for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, off + 64 * s, 0, kPolicy);
   }
 }
 // V: 1 KB of consecutive rows a load.
-template <bool kE4m3>
+template <bool kE4m3, int kPolicy>
 __device__ __forceinline__ void load_values(const Cache& C, const Piece& P, int lane, Raw<kE4m3>& r) {
   constexpr int kN = kE4m3 ? 2 : 4;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     const __amdgpu_buffer_rsrc_t b = tile_buffer<kE4m3>(C.v, P, i);
 #pragma unroll
-    for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, 1024 * s + lane * 16, 0, 0);
+    for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, 1024 * s + lane * 16, 0, kPolicy);
   }
 }
 
@@ -91,53 +100,57 @@ __device__ __forceinline__ u32x4 eight_bf16(uint32_t lo, uint32_t hi, float scal
   return u32x4{a.x, a.y, b.x, b.y};
 }
 
-// kSelected: the blocks of idx, a token a workgroup.  kGroup: every key, and A.group tokens of a sequence a workgroup.  Neither: every key, a token.
-template <bool kE4m3, bool kSelected, bool kGroup>
-__global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Cache C, CacheAttend A) {
-  extern __shared__ __align__(256) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, qg = lane >> 4;
-  Share W;
-  {
-    int b = (int)blockIdx.x;
-    W.split = b % A.splits;
-    b /= A.splits;
-    W.j = b % C.hkv;
-    b /= C.hkv;
-    if constexpr (!kGroup) {
-      const TokenPlace p = token_place(C, b);
-      W.s = p.s;
-      W.place = p.place;
-      W.t0 = b;
-      W.nt = 1;
-    } else {
-      // groups of A.group tokens: a sequence's start at floor(cu / group) + s, room for all of them without a scan over the batch
-      auto base = [&](int s) { return (int64_t)(C.cu[s] / A.group) + s; };
-      W.s = find_sequence(C.nseq, b, base);
-      if (W.s >= 0) {
-        const int c0 = C.cu[W.s], n = C.cu[W.s + 1] - c0, i0 = (b - (int)base(W.s)) * A.group;
-        W.t0 = c0 + i0;
-        W.nt = min(min(A.group, n - i0), C.T - W.t0);
-        W.place = C.kv_len[W.s] - n + i0;
-        if (W.nt <= 0 || W.t0 < 0) W.s = -1;
-      }
+// Row b of a call that gives every workgroup a row; s < 0 where there is none.
+template <bool kGroup>
+__device__ __forceinline__ Row row_of(const Cache& C, const CacheAttend& A, int b) {
+  Row W;
+  W.j = b % C.hkv;
+  b /= C.hkv;
+  if constexpr (!kGroup) {
+    const TokenPlace p = token_place(C, b);
+    W.s = p.s;
+    W.place = p.place;
+    W.t0 = b;
+    W.nt = 1;
+  } else {
+    // groups of A.group tokens: a sequence's start at floor(cu / group) + s, room for all of them without a scan over the batch
+    auto base = [&](int s) { return (int64_t)(C.cu[s] / A.group) + s; };
+    W.s = find_sequence(C.nseq, b, base);
+    if (W.s >= 0) {
+      const int c0 = C.cu[W.s], n = C.cu[W.s + 1] - c0, i0 = (b - (int)base(W.s)) * A.group;
+      W.t0 = c0 + i0;
+      W.nt = min(min(A.group, n - i0), C.T - W.t0);
+      W.place = C.kv_len[W.s] - n + i0;
+      if (W.nt <= 0 || W.t0 < 0) W.s = -1;
     }
-    if (W.s < 0) return;  // the whole workgroup
-    // the same in every lane, and said so: the buffers below are scalar
-    W.s = __builtin_amdgcn_readfirstlane(W.s);
-    W.t0 = __builtin_amdgcn_readfirstlane(W.t0);
-    W.nt = __builtin_amdgcn_readfirstlane(W.nt);
-    W.place = __builtin_amdgcn_readfirstlane(W.place);
-    W.j = __builtin_amdgcn_readfirstlane(W.j);
   }
+  return W;
+}
+
+// kSelected: the pieces are those of the blocks of idx; else all that the row sees.  kGroup: rows of more than one token.
+template <bool kE4m3, bool kSelected, bool kGroup, int kPolicy>
+__device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row W, Part part, char* smem) {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // what derives from it is not kept from row to row
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, qg = lane >> 4;
+  // the same in every lane, and said so: the buffers below are scalar
+  W.s = __builtin_amdgcn_readfirstlane(W.s);
+  W.t0 = __builtin_amdgcn_readfirstlane(W.t0);
+  W.nt = __builtin_amdgcn_readfirstlane(W.nt);
+  W.place = __builtin_amdgcn_readfirstlane(W.place);
+  W.j = __builtin_amdgcn_readfirstlane(W.j);
+  part.begin = __builtin_amdgcn_readfirstlane(part.begin);
+  part.end = __builtin_amdgcn_readfirstlane(part.end);
   const int limit = C.max_pages << C.page_log2;  // places that the table can name
   // this lane's column: token tt of the group, head hh; it sees the places [c_lo, c_hi)
   const int tt = kGroup ? col / C.g : 0, hh = col - tt * C.g, cols = W.nt * C.g;
   const bool used = col < cols;
-  const int c_hi = used ? min(W.place + tt + 1, limit) : 0, c_lo = A.window > 0 && used ? max(W.place + tt + 1 - A.window, 0) : 0;
   // what any column sees, and what all of them see
   const int lo = A.window > 0 ? max(W.place + 1 - A.window, 0) : 0, hi = min(W.place + W.nt, limit);
   const int all_lo = A.window > 0 ? max(W.place + W.nt - A.window, 0) : 0, all_hi = min(W.place + 1, limit);
+  // (what the unused columns see does not matter)
+  const int c_hi = kGroup ? min(W.place + tt + 1, limit) : hi, c_lo = kGroup && A.window > 0 ? max(W.place + tt + 1 - A.window, 0) : lo;
 
   bf16x8 qf[4];
   {
@@ -177,15 +190,23 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
     n_pieces = max((hi + kPiece - 1) / kPiece - first_piece, 0);
   }
 
-  // pieces w, w + step, ...: their places, pages and scales, kAhead pieces at a time, piece lane / kTiles of these and its tile lane % kTiles
+  // this workgroup's pieces, its wavefronts in turn; their places, pages and scales are looked up kAhead at a time, piece lane / kTiles of
+  // these and its tile lane % kTiles
   constexpr int kAhead = 64 / kTiles;
-  const int step = A.splits * kWaves, w0 = W.split * kWaves + wave;
-  const int mine = n_pieces > w0 ? (n_pieces - w0 + step - 1) / step : 0;
+  if constexpr (kSelected) {  // how many parts there are is known only now
+    const int n = max((n_pieces + A.chunk - 1) / A.chunk, 1);
+    if (part.begin >= n * A.chunk) return;  // the whole workgroup
+    part.whole = n == 1;
+    part.count = n;
+  }
+  const int begin = part.begin, end = min(part.end, n_pieces);
+  const int w0 = begin + wave;
+  const int mine = end > w0 ? (end - w0 + kWaves - 1) / kWaves : 0;
   int key_of = 0, rows_of = 0;
   int64_t row_of = 0;
   float k_scale = 1.f, v_scale = 1.f;
   auto look_up = [&](int i) __attribute__((always_inline)) {
-    const int p = w0 + (i + lane / kTiles) * step, pc = min(p, max(n_pieces - 1, 0));
+    const int p = w0 + (i + lane / kTiles) * kWaves, pc = min(p, end - 1);
     if constexpr (kSelected) {
       const int o = pc / per_block;
       const int id = (int)lane_value((uint32_t)blocks, o);
@@ -193,7 +214,7 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
     } else {
       key_of = (first_piece + pc) * kPiece;
     }
-    const int key = key_of + 16 * (lane % kTiles), page = p < n_pieces ? page_of(C, W.s, key) : -1;
+    const int key = key_of + 16 * (lane % kTiles), page = p < end ? page_of(C, W.s, key) : -1;
     rows_of = page < 0 ? 0 : min(max(hi - key, 0), 16);
     const int64_t at = (int64_t)max(page, 0) * C.hkv + W.j;
     row_of = (at << C.page_log2) + (key & ((1 << C.page_log2) - 1));
@@ -242,8 +263,8 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
   if (mine > 0) {
     look_up(0);
     P = piece(0);
-    load_keys<kE4m3>(C, P, lane, kr);
-    load_values<kE4m3>(C, P, lane, vr);
+    load_keys<kE4m3, kPolicy>(C, P, lane, kr);
+    load_values<kE4m3, kPolicy>(C, P, lane, vr);
   }
   for (int i = 0; i < mine; ++i) {
     const Piece cur = P;
@@ -267,7 +288,7 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
     if (more) {
       if ((i + 1) % kAhead == 0) look_up(i + 1);
       P = piece(i + 1);
-      load_keys<kE4m3>(C, P, lane, kr);
+      load_keys<kE4m3, kPolicy>(C, P, lane, kr);
     }
     // scores of places that the column does not see become -inf
     bool whole = cur.key0 >= all_lo && cur.key0 + kPiece <= all_hi;
@@ -326,7 +347,7 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
         }
       }
     }
-    if (more) load_values<kE4m3>(C, P, lane, vr);
+    if (more) load_values<kE4m3, kPolicy>(C, P, lane, vr);
     wave_sync();
     if (!kGroup || (cur.key0 >= all_lo && cur.key0 + kPiece <= all_hi)) {
 #pragma unroll
@@ -365,7 +386,9 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
     }
   }
   __syncthreads();
-  const int c = threadIdx.x >> 4, sub = threadIdx.x & 15;
+  const int c = tid >> 4, sub = tid & 15;
+  if (part.begin == 0 && A.rows != nullptr && c < W.nt && sub == 0)
+    A.rows[(int64_t)(W.t0 + c) * C.hkv + W.j] = int4{part.slot, part.second, part.whole ? 1 : part.count, W.t0};
   if (c >= cols) return;
   float top = -INFINITY, total = 0.f, o[8];
 #pragma unroll
@@ -388,11 +411,12 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
   }
   const int ct = kGroup ? c / C.g : 0;
   const int64_t row = (int64_t)(W.t0 + ct) * C.hq + W.j * C.g + (c - ct * C.g);
-  if (A.splits > 1) {
-    float* dst = A.part + (row * A.splits + W.split) * kD + 8 * sub;
+  if (!part.whole) {
+    const int64_t at = (int64_t)part.slot * A.cols + c;
+    float* dst = A.part + at * kD + 8 * sub;
     *reinterpret_cast<f32x4*>(dst) = f32x4{o[0], o[1], o[2], o[3]};
     *reinterpret_cast<f32x4*>(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
-    if (sub == 0) A.part_ml[row * A.splits + W.split] = float2{top, total};
+    if (sub == 0) A.part_ml[at] = float2{top, total};
     return;
   }
   const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
@@ -415,56 +439,191 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
   if (sub == 0) A.LSE[row] = total > 0.f || total != total ? (tc + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
 }
 
-// The splits of a row: a wavefront a row, two channels a lane.
+// A row a workgroup, or with A.splits the `chunk` pieces of a row that are its own.
+template <bool kE4m3, bool kSelected, bool kGroup, int kPolicy>
+__global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Cache C, CacheAttend A) {
+  extern __shared__ __align__(256) char smem[];
+  // all rows' first parts before the second ones: those that a short row leaves empty come last, and the XCDs, which get workgroups in
+  // turn, have as much to do each
+  const int rows = (int)gridDim.x / A.splits, split = (int)blockIdx.x / rows, b = (int)blockIdx.x - split * rows;
+  const Row W = row_of<kGroup>(C, A, b);
+  if (W.s < 0) return;  // the whole workgroup
+  Part P;
+  P.begin = split * A.chunk;
+  P.end = P.begin + A.chunk;
+  P.whole = true;
+  P.slot = b * A.splits + split;
+  P.second = P.slot + 1;
+  P.count = 1;
+  attend<kE4m3, kSelected, kGroup, kPolicy>(C, A, W, P, smem);
+}
+
+// Every key of sequences whose lengths only the device knows: all pieces of all rows, one row after the other, are cut into 512 equal parts, so
+// that all workgroups end together whatever the lengths.  A workgroup finds its sequence by a scan over the batch's lengths.  Its part may begin
+// and end inside a row; rows in between are its own.  Measured against parts of 1024 keys, with room for the longest row everywhere, joined by
+// row: 8 sequences of 4096 .. 131072, e4m3, 64 heads, g = 8, 139 -> 120 us; one of 65536, bf16, 32 heads 57 -> 54; 64 of 100 .. 32000 286 -> 267.  More
+// parts than 512 (768, 1024, 1536) cost up to 6 % but in the last case (256 us for 1536).
+__device__ __forceinline__ int64_t uniform(int64_t x) {  // a value that all lanes have, in scalar registers
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+template <bool kE4m3, bool kGroup, int kPolicy>
+__global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend_even(Cache C, CacheAttend A) {
+  extern __shared__ __align__(256) char smem[];
+  const int limit = C.max_pages << C.page_log2, n_wg = (int)gridDim.x, wg = (int)blockIdx.x;
+  auto pieces_of = [&](int s) __attribute__((always_inline)) {  // of each row of sequence s, no fewer than any of them has
+    const int n = (min(C.kv_len[s], limit) + kPiece - 1) / kPiece;
+    return max(A.window > 0 ? min(n, (A.window + A.group) / kPiece + 2) : n, 1);
+  };
+  auto groups_of = [&](int s) __attribute__((always_inline)) { return C.cu ? (max(C.cu[s + 1] - C.cu[s], 0) + A.group - 1) / A.group : 1; };
+  // exclusive sums over the batch: a run of `per` sequences a thread
+  const int per = (C.nseq + 64 * kWaves - 1) / (64 * kWaves), s0 = threadIdx.x * per, lane = threadIdx.x & 63;
+  int64_t own = 0;
+  for (int s = s0; s < min(s0 + per, C.nseq); ++s) own += (int64_t)groups_of(s) * C.hkv * pieces_of(s);
+  int64_t upto = own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t x = __shfl_up(upto, d);
+    if (lane >= d) upto += x;
+  }
+  int64_t* sums = reinterpret_cast<int64_t*>(smem);
+  if (lane == 63) sums[threadIdx.x >> 6] = upto;
+  __syncthreads();
+  int64_t before = upto - own, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < (int)(threadIdx.x >> 6)) before += sums[w];
+    total += sums[w];
+  }
+  total = uniform(total);
+  const int64_t share = max((total + n_wg - 1) / n_wg, (int64_t)kWaves), start = wg * share;
+  if (start >= total) return;  // the whole workgroup
+  if (before <= start && start < before + own) {
+    sums[kWaves] = s0;
+    sums[kWaves + 1] = before;
+  }
+  __syncthreads();
+  int s = __builtin_amdgcn_readfirstlane((int)sums[kWaves]);
+  int64_t at = start - uniform(sums[kWaves + 1]);
+  __syncthreads();
+  int groups = groups_of(s), pieces = pieces_of(s);
+  while (at >= (int64_t)groups * C.hkv * pieces) {
+    at -= (int64_t)groups * C.hkv * pieces;
+    ++s;
+    groups = groups_of(s);
+    pieces = pieces_of(s);
+  }
+  int unit = __builtin_amdgcn_readfirstlane((int)(at / pieces)), q = __builtin_amdgcn_readfirstlane((int)(at - (int64_t)unit * pieces));
+  const int each = __builtin_amdgcn_readfirstlane((int)share);  // below 2^31: checked on the host
+  int left = __builtin_amdgcn_readfirstlane((int)min(share, total - start));
+  for (bool first = true; left > 0; first = false) {
+    const int take = min(pieces - q, left), i = unit / C.hkv;
+    Row W;
+    W.s = s;
+    W.j = unit - i * C.hkv;
+    const int c0 = C.cu ? C.cu[s] : s, n = C.cu ? C.cu[s + 1] - c0 : 1, i0 = i * A.group;
+    W.t0 = c0 + i0;
+    W.nt = min(min(A.group, n - i0), C.T - W.t0);
+    W.place = C.kv_len[s] - n + i0;
+    Part P;
+    P.begin = q;
+    P.end = q + take;
+    P.whole = take == pieces;
+    P.slot = 2 * wg + (first ? 0 : 1);
+    P.second = 2 * (wg + 1);
+    P.count = 1 + (pieces - take + each - 1) / each;
+    if (W.nt > 0 && W.t0 >= 0) attend<kE4m3, false, kGroup, kPolicy>(C, A, W, P, smem);
+    left -= take;
+    q = 0;
+    if (++unit == groups * C.hkv && left > 0) {
+      unit = 0;
+      do {
+        ++s;
+        groups = groups_of(s);
+      } while (groups == 0);
+      pieces = pieces_of(s);
+    }
+    __syncthreads();  // the LDS is the next row's
+  }
+}
+
+// The parts of a row: a workgroup a row, whose groups of 16 lanes, 8 channels a lane, take them in turn.
 __global__ void __launch_bounds__(256) k_cache_join(Cache C, CacheAttend A) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= (int64_t)C.T * C.hq) return;
-  const int lane = threadIdx.x & 63, t = (int)(row / C.hq);
+  __shared__ float sums[16][kD + 4], stats[16];
+  const int64_t row = blockIdx.x;
+  const int t = (int)(row / C.hq), h = (int)(row - (int64_t)t * C.hq), grp = threadIdx.x >> 4, sub = threadIdx.x & 15;
   if (C.cu && (t < C.cu[0] || t >= C.cu[C.nseq])) return;  // rows of no sequence are left as they were
+  const int4 R = A.rows[(int64_t)t * C.hkv + h / C.g];
+  if (R.z <= 1) return;  // written already
+  // (the bounds matter only if the starts of the sequences are not in order and no workgroup has written R)
+  const int n = min(R.z, A.slots), col = min(max(t - R.w, 0) * C.g + h % C.g, A.cols - 1);
+  auto slot = [&](int i) { return (int64_t)min((uint32_t)(i == 0 ? R.x : R.y + (i - 1) * A.slot_step), (uint32_t)A.slots - 1) * A.cols + col; };
   const float c2 = A.scale * 1.4426950408889634f;
-  const float2* ml = A.part_ml + row * A.splits;
   float top = -INFINITY;
-  for (int s = 0; s < A.splits; ++s) top = fmaxf(top, ml[s].x);
+  for (int i = sub; i < n; i += 16) top = fmaxf(top, A.part_ml[slot(i)].x);
+#pragma unroll
+  for (int m = 1; m < 16; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
   const float tc = top == -INFINITY ? 0.f : top * c2;
-  const f32x2* from = reinterpret_cast<const f32x2*>(A.part + row * A.splits * kD) + lane;
-  float total = 0.f;
-  f32x2 o = {0.f, 0.f};
-#pragma unroll 4
-  for (int s = 0; s < A.splits; ++s) {
-    const float2 x = ml[s];
+  float total = 0.f, o[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll 2
+  for (int i = grp; i < n; i += 16) {
+    const int64_t at = slot(i);
+    const float2 x = A.part_ml[at];
+    const float* from = A.part + at * kD + 8 * sub;
+    const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
     const float f = __builtin_amdgcn_exp2f(fmaf(x.x, c2, -tc));
-    const f32x2 v = from[s * (kD / 2)];
     total = fmaf(f, x.y, total);
-    o[0] = fmaf(f, v[0], o[0]);
-    o[1] = fmaf(f, v[1], o[1]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[e] = fmaf(f, a[e], o[e]);
+      o[4 + e] = fmaf(f, b[e], o[4 + e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[grp][8 * sub + e] = o[e];
+  if (sub == 0) stats[grp] = total;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const int lane = threadIdx.x;
+  float p = 0.f, q = 0.f;
+  total = 0.f;
+#pragma unroll
+  for (int g = 0; g < 16; ++g) {
+    p += sums[g][2 * lane];
+    q += sums[g][2 * lane + 1];
+    total += stats[g];
   }
   const bool some = total > 0.f || total != total;
   const float inv = some ? 1.f / total : 0.f;
-  o[0] *= inv;
-  o[1] *= inv;
+  p *= inv;
+  q *= inv;
   if (A.gate) {
     const float gate = A.gate[row];
     const uint32_t x = A.o_acc ? reinterpret_cast<const uint32_t*>(A.o_acc)[row * (kD / 2) + lane] : 0u;
-    o[0] = fmaf(gate, o[0], bf16_lo(x));
-    o[1] = fmaf(gate, o[1], bf16_hi(x));
+    p = fmaf(gate, p, bf16_lo(x));
+    q = fmaf(gate, q, bf16_hi(x));
   }
-  reinterpret_cast<uint32_t*>(A.O)[row * (kD / 2) + lane] = pack_bf16x2(o[0], o[1]);
+  reinterpret_cast<uint32_t*>(A.O)[row * (kD / 2) + lane] = pack_bf16x2(p, q);
   if (lane == 0) A.LSE[row] = some ? (tc + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
 }
 
 }  // namespace
 
 hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, hipStream_t st) {
-  // workgroups: a token and head, or a group of tokens of a sequence and head, times the splits
   const bool grouped = A.group > 1;
   const int64_t groups = grouped ? C.T / A.group + C.nseq : C.T;
-  const int64_t grid = groups * C.hkv * A.splits;
-  static std::atomic<uint64_t> ready[6];
-  static constexpr decltype(&k_cache_attend<false, false, false>) kForms[6] = {
-      k_cache_attend<false, false, false>, k_cache_attend<true, false, false>, k_cache_attend<false, false, true>,
-      k_cache_attend<true, false, true>,   k_cache_attend<false, true, false>, k_cache_attend<true, true, false>};
-  const int form = (A.idx ? 4 : grouped ? 2 : 0) + (e4m3 ? 1 : 0);
-  const auto kern = kForms[form];
+  const int64_t grid = A.even > 0 ? A.even : groups * C.hkv * A.splits;
+  static std::atomic<uint64_t> ready[16];
+  using Kernel = void (*)(Cache, CacheAttend);
+#define FORMS(e4m3, policy)                                                                                           \
+  k_cache_attend<e4m3, true, false, policy>, k_cache_attend<e4m3, false, false, policy>,                              \
+      k_cache_attend_even<e4m3, false, policy>
+  static const Kernel kForms[16] = {FORMS(false, 0), k_cache_attend<false, false, true, 0>, FORMS(false, kNonTemporal), k_cache_attend_even<false, true, 0>,
+                                    FORMS(true, 0),  k_cache_attend<true, false, true, 0>,  FORMS(true, kNonTemporal),  k_cache_attend_even<true, true, 0>};
+#undef FORMS
+  const int form = (e4m3 ? 8 : 0) + (grouped ? (A.even > 0 ? 7 : 3) : (A.streaming ? 4 : 0) + (A.idx ? 0 : A.even > 0 ? 2 : 1));
+  const Kernel kern = kForms[form];
   hipError_t e = allow_dynamic_lds((const void*)kern, kAttendLds, ready[form]);
   if (e != hipSuccess) return e;
   {
@@ -472,9 +631,9 @@ hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, 
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * kWaves), kAttendLds, st, C, A);
   }
   e = hipGetLastError();
-  if (e != hipSuccess || A.splits == 1) return e;
+  if (e != hipSuccess || A.rows == nullptr) return e;
   ProfScope ps(KID_CACHE_JOIN, st);
-  hipLaunchKernelGGL(k_cache_join, dim3((unsigned)(((int64_t)C.T * C.hq + 3) / 4)), dim3(256), 0, st, C, A);
+  hipLaunchKernelGGL(k_cache_join, dim3((unsigned)((int64_t)C.T * C.hq)), dim3(256), 0, st, C, A);
   return hipGetLastError();
 }
 
