@@ -240,12 +240,16 @@ def select_blocks(scores: torch.Tensor, cu: Optional[torch.Tensor], topk: int, *
         nseq = kv_len.numel()
         if cu is None and nseq != T:
             raise NsaSelError(f"without cu_seqlens every sequence has one new token: {nseq} lengths for {T} tokens")
-        if out is None:
-            out = torch.empty(T, hkv, topk, dtype=torch.int32, device=dev) if cu is None else torch.full((T, hkv, topk), -1, dtype=torch.int32, device=dev)
-        expect_tensor("scores", scores, torch.float32, (T, hkv, stride), dev)
+        if out is not None:
+            expect_tensor("out", out, torch.int32, (T, hkv, topk), dev)
+        elif cu is None:
+            out = torch.empty((T, hkv, topk), dtype=torch.int32, device=dev)
+        else:
+            out = torch.full((T, hkv, topk), -1, dtype=torch.int32, device=dev)
+        if not scores.is_contiguous():
+            raise NsaSelError("scores must be contiguous")
         expect_tensor("cu_seqlens", cu, torch.int32, (nseq + 1,), dev, optional=True)
         expect_tensor("kv_len", kv_len, torch.int32, (nseq,), dev)
-        expect_tensor("out", out, torch.int32, (T, hkv, topk), dev)
         shape = CacheShape(T, nseq, hkv, hkv, 128, 0, 64, 0, 0, block, topk, 0, 0.0)
         _launch(lib().nsa_sel_select_blocks_cached, "nsa_sel_select_blocks_cached", dev, C.byref(shape), _ptr(scores), stride, _ptr(cu),
                 _ptr(kv_len), n_sink, n_local, _ptr(out))

@@ -9,6 +9,9 @@ import torch
 
 from .binding import CacheShape, NsaSelError, _check, _device, _launch, _ptr, expect_tensor, expect_workspace, lib
 
+# A decoding loop calls these a few times a layer with a few tokens: what a call costs on the host is what it costs.  So a tensor is looked at
+# once, and what follows from the sizes of a call alone is kept for the next call of the same sizes.
+
 _BF16, _F32, _I32, _F64 = torch.bfloat16, torch.float32, torch.int32, torch.float64
 _D = 128
 
@@ -32,12 +35,6 @@ def _rows(name: str, t, shape, device) -> int:
     if tokens > 1 and (each < heads * _D or each & 7):
         raise NsaSelError(f"the tokens of {name} must be a multiple of 8 values apart, and not overlap")
     return each if tokens > 1 else heads * _D
-
-
-def _dims(name: str, t, n: int):
-    if not isinstance(t, torch.Tensor) or t.dim() != n:
-        raise NsaSelError(f"{name} must be a torch.Tensor of {n} dimensions")
-    return t.shape
 
 
 class PagedCache:
@@ -92,18 +89,35 @@ class PagedCache:
         self.n_pages, self.hkv, self.page, self.device = n_pages, hkv, page, k_pages.device
         self._dtype = 1 if e4m3 else 0
         self._pointers = tuple(_ptr(t) for t in (k_pages, v_pages, k_scale, v_scale))
+        self._shapes = {}  # sizes of a call -> (its shape, bytes of its workspace)
 
     def _batch(self, tokens: int, table, kv_len, cu) -> Tuple[int, int]:
         """(sequences, columns of table) after the checks that all calls share."""
         dev = self.device
-        nseq, max_pages = _dims("table", table, 2)
-        expect_tensor("table", table, _I32, table.shape, dev)
+        try:
+            nseq, max_pages = table.shape
+        except (AttributeError, ValueError):
+            raise NsaSelError("table must be int32 [sequences, max_pages]") from None
+        expect_tensor("table", table, _I32, (nseq, max_pages), dev)
         expect_tensor("kv_len", kv_len, _I32, (nseq,), dev)
         if cu is not None:
             expect_tensor("cu_seqlens", cu, _I32, (nseq + 1,), dev)
         elif nseq != tokens:
             raise NsaSelError(f"without cu_seqlens every sequence has one new token: {nseq} sequences for {tokens} tokens")
         return nseq, max_pages
+
+    def _shape(self, tokens, nseq, hq, max_pages, block=64, topk=0, window=0, scale=0.0):
+        """The shape of a call, to be passed on, and the bytes of the attention's workspace."""
+        key = (tokens, nseq, hq, max_pages, block, topk, window, scale)
+        known = self._shapes.get(key)
+        if known is None:
+            shape = CacheShape(tokens, nseq, hq, self.hkv, _D, self._dtype, self.page, self.n_pages, max_pages, block, topk, window, scale)
+            need = C.c_size_t()
+            _check(lib().nsa_sel_cache_workspace_bytes(C.byref(shape), C.byref(need)), "nsa_sel_cache_workspace_bytes")
+            if len(self._shapes) >= 4096:
+                self._shapes.clear()
+            known = self._shapes[key] = (C.byref(shape), need.value)
+        return known
 
     def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
                q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
@@ -116,43 +130,46 @@ class PagedCache:
         attention.  q_out / k_out take the results (they may be q / k themselves if those are contiguous); rows of tokens that belong to no
         sequence are left as they are there, and uninitialised otherwise."""
         dev, hkv = self.device, self.hkv
-        T = _dims("k", k, 3)[0]
-        k_stride, v_stride = _rows("k", k, (T, hkv, _D), dev), _rows("v", v, (T, hkv, _D), dev)
+        try:
+            T = k.shape[0]
+        except (AttributeError, IndexError):
+            raise NsaSelError("k must be bfloat16 [tokens, hkv, 128]") from None
+        kv_rows = (T, hkv, _D)
+        k_stride, v_stride = _rows("k", k, kv_rows, dev), _rows("v", v, kv_rows, dev)
         nseq, max_pages = self._batch(T, table, kv_len, cu)
         hq, rot, q_stride, q_ptr = hkv, 0, 0, None
         if q is not None:
-            hq = _dims("q", q, 3)[1]
+            try:
+                _, hq, _ = q.shape
+            except (AttributeError, ValueError):
+                raise NsaSelError("q must be bfloat16 [tokens, hq, 128]") from None
             rows = (T, hq, _D)
             q_stride, q_ptr = _rows("q", q, rows, dev), q.data_ptr()
             if q_out is None:
-                q_out = torch.empty(rows, dtype=_BF16, device=dev)
+                q_out = torch.empty_like(q) if q_stride == hq * _D else torch.empty(rows, dtype=_BF16, device=dev)
             else:
                 expect_tensor("q_out", q_out, _BF16, rows, dev)
         elif q_out is not None:
             raise NsaSelError("q_out without q")
         if k_out is not None:
-            expect_tensor("k_out", k_out, _BF16, (T, hkv, _D), dev)
+            expect_tensor("k_out", k_out, _BF16, kv_rows, dev)
         elif rotated_k:
-            k_out = torch.empty((T, hkv, _D), dtype=_BF16, device=dev)
+            k_out = torch.empty(kv_rows, dtype=_BF16, device=dev)
         if inv_freq is not None:
-            pairs = _dims("inv_freq", inv_freq, 1)[0]
+            try:
+                pairs, = inv_freq.shape
+            except (AttributeError, ValueError):
+                raise NsaSelError("inv_freq must be float64 [rot / 2]") from None
             expect_tensor("inv_freq", inv_freq, _F64, (pairs,), dev)
             rot = 2 * pairs
-        shape = CacheShape(T, nseq, hq, hkv, _D, self._dtype, self.page, self.n_pages, max_pages, 64, 0, 0, 0.0)
-        _launch(lib().nsa_sel_cache_append, "nsa_sel_cache_append", dev, C.byref(shape), q_ptr, q_stride, k.data_ptr(), k_stride,
+        _launch(lib().nsa_sel_cache_append, "nsa_sel_cache_append", dev, self._shape(T, nseq, hq, max_pages)[0], q_ptr, q_stride, k.data_ptr(), k_stride,
                 v.data_ptr(), v_stride, _ptr(cu), kv_len.data_ptr(), table.data_ptr(), _ptr(inv_freq), rot, int(interleaved),
                 *self._pointers, _ptr(q_out), _ptr(k_out))
         return q_out, k_out
 
     def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
         """Bytes that attention() of such a call needs as `ws`."""
-        return self._ws_bytes(CacheShape(tokens, nseq, hq, self.hkv, _D, self._dtype, self.page, self.n_pages, max_pages, block, topk, window, 0.0))
-
-    @staticmethod
-    def _ws_bytes(shape) -> int:
-        n = C.c_size_t()
-        _check(lib().nsa_sel_cache_workspace_bytes(C.byref(shape), C.byref(n)), "nsa_sel_cache_workspace_bytes")
-        return n.value
+        return self._shape(tokens, nseq, hq, max_pages, block, topk, window)[1]
 
     def attention(self, q: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
                   idx: Optional[torch.Tensor] = None, block: int = 64, window: int = 0, scale: float = 0.0,
@@ -165,15 +182,21 @@ class PagedCache:
         out / lse take the results (out may be o_acc); rows of tokens that belong to no sequence are left as they are there, and
         uninitialised otherwise.  ws, of workspace_bytes(), is for callers that may not allocate."""
         dev = self.device
-        T, hq, _ = _dims("q", q, 3)
+        try:
+            T, hq, _ = q.shape
+        except (AttributeError, ValueError):
+            raise NsaSelError("q must be bfloat16 [tokens, hq, 128]") from None
         rows = (T, hq, _D)
         expect_tensor("q", q, _BF16, rows, dev)
         nseq, max_pages = self._batch(T, table, kv_len, cu)
         topk = 0
         if idx is not None:
-            topk = _dims("idx", idx, 3)[2]
+            try:
+                _, _, topk = idx.shape
+            except (AttributeError, ValueError):
+                topk = 0
             if topk < 1:
-                raise NsaSelError("idx must have a column")
+                raise NsaSelError("idx must be int32 [tokens, hkv, topk], topk at least 1")
             expect_tensor("idx", idx, _I32, (T, self.hkv, topk), dev)
         if gate is not None:
             expect_tensor("gate", gate, _F32, (T, hq), dev)
@@ -182,20 +205,19 @@ class PagedCache:
         elif o_acc is not None:
             raise NsaSelError("o_acc without gate")
         if out is None:
-            out = torch.empty(rows, dtype=_BF16, device=dev)
+            out = torch.empty_like(q)
         else:
             expect_tensor("out", out, _BF16, rows, dev)
         if lse is None:
             lse = torch.empty((T, hq), dtype=_F32, device=dev)
         else:
             expect_tensor("lse", lse, _F32, (T, hq), dev)
-        shape = CacheShape(T, nseq, hq, self.hkv, _D, self._dtype, self.page, self.n_pages, max_pages, block, topk, window, scale)
-        need = self._ws_bytes(shape)
+        shape, need = self._shape(T, nseq, hq, max_pages, block, topk, window, scale)
         if ws is not None:
             expect_workspace("ws", ws, need, dev)
         elif need:
             ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        _launch(lib().nsa_sel_cache_attention, "nsa_sel_cache_attention", dev, C.byref(shape), q.data_ptr(), _ptr(idx), _ptr(cu),
+        _launch(lib().nsa_sel_cache_attention, "nsa_sel_cache_attention", dev, shape, q.data_ptr(), _ptr(idx), _ptr(cu),
                 kv_len.data_ptr(), table.data_ptr(), *self._pointers, _ptr(gate), _ptr(o_acc), out.data_ptr(), lse.data_ptr(), _ptr(ws),
                 0 if ws is None else need)
         return out, lse

@@ -100,13 +100,15 @@ __device__ __forceinline__ int place_of_pair(const Rotation& R, int p) {
 
 // ---- rows of tokens: queries, and the keys and values of a bf16 cache ------------------------------------------------------------------
 // A workgroup takes the rows of kTokens consecutive tokens from t0, or with `parts` every parts-th step of them.  A thread requests
-// kBatch rows before it waits for the angles.
+// kBatch rows before it waits for the angles.  Written with non-temporal stores: 32768 tokens, 32 + 2 x 8 heads, 805 MB 160 -> 152 us (5.3 TB/s; a copy
+// of 1 GB runs at 5.1), 2048 tokens 11.8 -> 10.3; non-temporal loads gain only apart (168 -> 156 us with the pages' launch, 32768 tokens), and
+// four tokens a workgroup only among pages in 8 bits (bf16: 2048 tokens 11.7 -> 14.8).
 template <int kTokens>
 struct RowsLds {
   float2 cs[kTokens * kMaxPairs];
   int place[kTokens], page[kTokens];  // place < 0: nothing to do
 };
-template <int kThreads, int kTokens, bool kStore>
+template <int kThreads, int kTokens, bool kStore, bool kApart = false>
 __device__ __forceinline__ void token_rows(const Cache& C, const AppendArgs& A, int t0, int part, int parts, RowsLds<kTokens>& L) {
   constexpr int kRowsAtOnce = kThreads / 16, kBatch = 4;
   static_assert(kTokens <= kThreads / 64, "a wavefront a token");
@@ -135,7 +137,7 @@ __device__ __forceinline__ void token_rows(const Cache& C, const AppendArgs& A, 
     const int64_t t = t0 + k;
     const bf16_t* src = h < nq ? A.Q + t * A.q_stride + h * kD
                         : h < nq + C.hkv ? A.K + t * A.k_stride + (h - nq) * kD : A.V + t * A.v_stride + (h - nq - C.hkv) * kD;
-    return *reinterpret_cast<const u32x4*>(src + 8 * sub);
+    return kApart ? load_streaming(src + 8 * sub) : *reinterpret_cast<const u32x4*>(src + 8 * sub);
   };
   const int step = parts * kRowsAtOnce;
   for (int at = part * kRowsAtOnce; at < rows; at += kBatch * step) {  // the same for the whole workgroup
@@ -156,25 +158,26 @@ __device__ __forceinline__ void token_rows(const Cache& C, const AppendArgs& A, 
       const int place = L.place[k];
       if (rn >= rows || place < 0) continue;
       if (is_q) {
-        *reinterpret_cast<u32x4*>(A.Q_out + (t * C.hq + h) * kD + 8 * sub) = y;
+        store_streaming(A.Q_out + (t * C.hq + h) * kD + 8 * sub, y);
         continue;
       }
       if constexpr (kStore) {
         const int j = is_k ? h - nq : h - nq - C.hkv, page = L.page[k];
-        if (is_k && A.K_out) *reinterpret_cast<u32x4*>(A.K_out + (t * C.hkv + j) * kD + 8 * sub) = y;
+        if (is_k && A.K_out) store_streaming(A.K_out + (t * C.hkv + j) * kD + 8 * sub, y);
         if (page >= 0) {
           const int64_t row = (((int64_t)page * C.hkv + j) << C.page_log2) + (place & ((1 << C.page_log2) - 1));
-          *reinterpret_cast<u32x4*>((is_k ? C.k : C.v) + row * (2 * kD) + 16 * sub) = y;
+          store_streaming(reinterpret_cast<bf16_t*>(is_k ? C.k : C.v) + row * kD + 8 * sub, y);
         }
       }
     }
   }
 }
 
+// kStore: with the keys and values of a bf16 cache.  Else the query rows apart, where the pages in 8 bits fill a launch of their own.
 template <int kTokens, bool kStore>
 __global__ void __launch_bounds__(kRowThreads) k_cache_append_rows(Cache C, AppendArgs A) {
   __shared__ RowsLds<kTokens> L;
-  token_rows<kRowThreads, kTokens, kStore>(C, A, (int)blockIdx.x * kTokens, (int)blockIdx.y, (int)gridDim.y, L);
+  token_rows<kRowThreads, kTokens, kStore, !kStore>(C, A, (int)blockIdx.x * kTokens, (int)blockIdx.y, (int)gridDim.y, L);
 }
 
 // ---- pages in 8 bits -----------------------------------------------------------------------------------------------------------
@@ -189,17 +192,16 @@ __device__ __forceinline__ int exponent_of(float s) { return (int)((__builtin_bi
 
 // 8 values in the page's scale as e4m3, rounded to nearest.  What is beyond 448 after scaling (values of 2^127 and more) saturates;
 // infinities and NaN become NaN.
-__device__ __forceinline__ uint2 to_e4m3(const float (&f)[8], float inverse) {
+__device__ __forceinline__ uint64_t to_e4m3(const float (&f)[8], float inverse) {
   float y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float z = fminf(fmaxf(f[i] * inverse, -448.f), 448.f);
     y[i] = __builtin_fabsf(f[i]) < __builtin_inff() ? z : __builtin_nanf("");
   }
-  uint2 r;
-  r.x = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
-  r.y = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false), true);
-  return r;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false), true);
+  return (uint64_t)hi << 32 | lo;
 }
 // Four e4m3 values times a power of two, rounded again.
 __device__ __forceinline__ uint32_t rescale_e4m3(uint32_t x, float by) {
@@ -287,7 +289,7 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
       else unpack(x[i], f[i]);
       if (r >= rows) continue;
       if (kKey && write && A.K_out)
-        *reinterpret_cast<u32x4*>(A.K_out + ((int64_t)(U.t0 + tile * kTileRows + r) * C.hkv + h) * kD + 8 * sub) = pack(f[i]);
+        store_streaming(A.K_out + ((int64_t)(U.t0 + tile * kTileRows + r) * C.hkv + h) * kD + 8 * sub, pack(f[i]));
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float a = __builtin_fabsf(f[i][e]);
@@ -332,7 +334,7 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       const int r = i * kRowsAtOnce + rg;
-      if (r < rows_of(tile)) *reinterpret_cast<uint2*>(to + r * kD) = to_e4m3(f[i], inverse);
+      if (r < rows_of(tile)) __builtin_nontemporal_store(to_e4m3(f[i], inverse), reinterpret_cast<uint64_t*>(to + r * kD));
     }
   };
   // a head after the other; a page of one tile in one step, else its tiles twice: for the largest magnitude, and to be stored
@@ -409,10 +411,10 @@ hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t
     hipLaunchKernelGGL(kern, dim3((unsigned)((C.T + tokens - 1) / tokens), (unsigned)parts), dim3(kRowThreads), 0, st, C, A);
     return hipGetLastError();
   };
-  // rows of tokens: four tokens a workgroup where that still fills the chip, else a token's rows over as many as 512 of them
   const bool many = C.T >= 4096;
+  // a token's rows over as many as 512 workgroups
   auto parts_of = [&](int at_once) { return std::max(1, std::min((each + at_once - 1) / at_once, 512 / C.T)); };
-  if (!e4m3) return many ? rows(k_cache_append_rows<4, true>, 4, 1) : rows(k_cache_append_rows<1, true>, 1, parts_of(kRowThreads / 16));
+  if (!e4m3) return rows(k_cache_append_rows<1, true>, 1, parts_of(kRowThreads / 16));
   // Pages in 8 bits.  Heads of a page share its angles where that leaves workgroups enough; and where the pages by themselves fill the chip
   // the query rows, which want more wavefronts than pages leave registers for, are a launch of their own.  (us, 32768 tokens, 32 + 8
   // heads: one launch, a head a workgroup 186 -> 167, in pages of 256 tokens 214 -> 185; 16000 tokens, 8 + 8 heads 69 -> 54; but 5900 tokens

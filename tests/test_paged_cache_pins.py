@@ -78,7 +78,7 @@ ODD = C.c_void_p(4104)
 
 def _shape(nsa, **kw):
     from paper_2508_18224_amd.binding import CacheShape
-    d = dict(n_tokens=4, nseq=4, hq=8, hkv=2, d=128, dtype=1, page=64, n_pages=10, max_pages=3, block=64, topk=4, window=0, scale=0.0)
+    d = dict(n_tokens=4, nseq=4, hq=8, hkv=2, d=128, dtype=1, page=64, n_pages=10, max_pages=30, block=64, topk=16, window=0, scale=0.0)
     d.update(kw)
     return CacheShape(*[d[n] for n, _ in CacheShape._fields_])
 
