@@ -49,7 +49,6 @@ struct Piece {
   int key0;            // place of its first key
   int64_t row[kTiles];   // of the pages' rows, its first
   int rows[kTiles];      // that anything of the workgroup sees; 0 where there is no page
-  float ks[kTiles], vs[kTiles];
 };
 __device__ __forceinline__ float lane_float(float x, int l) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l));
@@ -127,9 +126,9 @@ __device__ __forceinline__ Row row_of(const Cache& C, const CacheAttend& A, int 
   return W;
 }
 
-// kSelected: the pieces are those of the blocks of idx; else all that the row sees.  kGroup: rows of more than one token.
+// kSelected: the pieces are those of the blocks of idx, whose column `my` of the row this lane has; else all that the row sees.  kGroup: rows of more than one token.
 template <bool kE4m3, bool kSelected, bool kGroup, int kPolicy>
-__device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row W, Part part, char* smem) {
+__device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row W, Part part, int my, char* smem) {
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));  // what derives from it is not kept from row to row
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -169,7 +168,6 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
   int n_pieces, first_piece = 0, blocks = 0;
   const int per_block = A.block / kPiece;
   if constexpr (kSelected) {
-    const int my = lane < A.topk ? A.idx[((int64_t)W.t0 * C.hkv + W.j) * A.topk + lane] : -1;
     const int64_t b0 = (int64_t)my * A.block;
     const bool ok = my >= 0 && b0 < hi && b0 + A.block > lo;
     const uint64_t okm = __builtin_amdgcn_ballot_w64(ok);
@@ -234,8 +232,6 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
       P.rows[x] = __builtin_amdgcn_readlane(rows_of, l + x);
       P.row[x] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(row_of >> 32), l + x) << 32 |
                            (uint32_t)__builtin_amdgcn_readlane((int)row_of, l + x));
-      P.ks[x] = kE4m3 ? lane_float(k_scale, l + x) : 1.f;
-      P.vs[x] = kE4m3 ? lane_float(v_scale, l + x) : 1.f;
     }
     return P;
   };
@@ -268,6 +264,12 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
   }
   for (int i = 0; i < mine; ++i) {
     const Piece cur = P;
+    float ks[kTiles], vs[kTiles];  // (taken here and not with the piece: its loads need not wait for those of the scales)
+#pragma unroll
+    for (int x = 0; x < kTiles; ++x) {
+      ks[x] = kE4m3 ? lane_float(k_scale, (i % kAhead) * kTiles + x) : 1.f;
+      vs[x] = kE4m3 ? lane_float(v_scale, (i % kAhead) * kTiles + x) : 1.f;
+    }
     f32x4 sacc[kTiles];
 #pragma unroll
     for (int x = 0; x < kTiles; ++x) {
@@ -277,7 +279,7 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
         u32x4 a;
         if constexpr (kE4m3) {
           const u32x4 r = kr.x[2 * x + (s >> 1)];
-          a = (s & 1) ? eight_bf16(r[2], r[3], cur.ks[x]) : eight_bf16(r[0], r[1], cur.ks[x]);
+          a = (s & 1) ? eight_bf16(r[2], r[3], ks[x]) : eight_bf16(r[0], r[1], ks[x]);
         } else {
           a = kr.x[4 * x + s];
         }
@@ -340,8 +342,8 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
         if (cur.key0 + row + w_row < lo) r = u32x4{0u, 0u, 0u, 0u};
         const uint32_t at = (wa ^ (row_turn(row) << 4)) + row * kVRow;
         if constexpr (kE4m3) {
-          lds_write_16(at, eight_bf16(r[0], r[1], cur.vs[x]));
-          lds_write_16(at ^ 16, eight_bf16(r[2], r[3], cur.vs[x]));
+          lds_write_16(at, eight_bf16(r[0], r[1], vs[x]));
+          lds_write_16(at ^ 16, eight_bf16(r[2], r[3], vs[x]));
         } else {
           lds_write_16(at, r);
         }
@@ -446,6 +448,8 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
   // all rows' first parts before the second ones: those that a short row leaves empty come last, and the XCDs, which get workgroups in
   // turn, have as much to do each
   const int rows = (int)gridDim.x / A.splits, split = (int)blockIdx.x / rows, b = (int)blockIdx.x - split * rows;
+  // this lane's column of idx, requested before the sequence and its length are known
+  const int lane = threadIdx.x & 63, my = kSelected && lane < A.topk ? A.idx[(int64_t)b * A.topk + lane] : -1;
   const Row W = row_of<kGroup>(C, A, b);
   if (W.s < 0) return;  // the whole workgroup
   Part P;
@@ -455,7 +459,7 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend(Ca
   P.slot = b * A.splits + split;
   P.second = P.slot + 1;
   P.count = 1;
-  attend<kE4m3, kSelected, kGroup, kPolicy>(C, A, W, P, smem);
+  attend<kE4m3, kSelected, kGroup, kPolicy>(C, A, W, P, my, smem);
 }
 
 // Every key of sequences whose lengths only the device knows: all pieces of all rows, one row after the other, are cut into 512 equal parts, so
@@ -531,7 +535,7 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend_ev
     P.slot = 2 * wg + (first ? 0 : 1);
     P.second = 2 * (wg + 1);
     P.count = 1 + (pieces - take + each - 1) / each;
-    if (W.nt > 0 && W.t0 >= 0) attend<kE4m3, false, kGroup, kPolicy>(C, A, W, P, smem);
+    if (W.nt > 0 && W.t0 >= 0) attend<kE4m3, false, kGroup, kPolicy>(C, A, W, P, -1, smem);
     left -= take;
     q = 0;
     if (++unit == groups * C.hkv && left > 0) {

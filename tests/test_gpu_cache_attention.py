@@ -162,3 +162,64 @@ def test_no_tokens():
     assert o.shape == (0, 4, 128) and l.shape == (0, 4)
     o, l = cache.attention(empty, b.dtable, b.dlen, torch.zeros(2, dtype=torch.int32, device="cuda"))
     assert o.shape == (0, 4, 128)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("kv,new,hq,hkv,page,window", [
+    ([int(1.21 ** i) for i in range(1, 42)], None, 8, 4, 16, 0),                         # parts that end inside rows and span several
+    ([2500, 3, 0, 1400, 77, 2000, 1, 1], [5, 3, 0, 2, 9, 1, 1, 0], 8, 2, 64, 0),         # the same with groups of tokens
+    ([1 + 11 * (i % 7) for i in range(300)] + [1600], None, 4, 1, 32, 0),                # more sequences than threads
+    ([3000, 1000, 1700], None, 4, 2, 16, 1500), ([2600, 90], [7, 30], 16, 2, 128, 1400), ([40000], None, 8, 1, 256, 0)])
+def test_every_key_cut_evenly(kv, new, hq, hkv, page, window, e4m3):
+    b = Batch(len(kv) + hq, kv, new, hq=hq, hkv=hkv, page=page, e4m3=e4m3, pad=0 if new is None else 2)
+    assert b.table.shape[1] * page > 40 * 32 and (not window or window > 40 * 32)
+    _run(b, window=window, gate=True)
+
+
+def test_more_sequences_than_are_cut_evenly():
+    """Every sequence is a workgroup's where a scan over the batch would cost more than it gives; a long table all the same."""
+    b = Batch(41, [i % 50 for i in range(4100)] , hq=2, hkv=1, page=16)
+    b.table = np.concatenate([b.table, np.full((4100, 100), -1, dtype=np.int32)], 1)
+    _run(b)
+
+
+def _shared(b, n, lens):
+    """n sequences over the pages of the only one of `b`: prefixes of it."""
+    rng = np.random.default_rng(42)
+    b.table, b.kv_len = np.repeat(b.table, n, 0), np.array(lens, dtype=np.int32)
+    b.T = n
+    b.q = np.asarray(np.repeat(b.q, n, 0) * rng.choice([-1.0, -0.5, 0.5, 1.0], (n, b.hq, 128)))
+    b.k, b.v = np.repeat(b.k, n, 0), np.repeat(b.v, n, 0)
+    return b
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_large_calls_over_shared_pages(e4m3):
+    """Calls that read more than 96 MB, by which the reads are requested otherwise: selected blocks in parts, a window of many rows, every key."""
+    rng = np.random.default_rng(43)
+    b = _shared(Batch(44, [5000], hq=8, hkv=2, page=64, e4m3=e4m3), 60, [4100 + 15 * i for i in range(60)])
+    idx = np.stack([np.stack([rng.permutation(32) for _ in range(2)]) for _ in range(60)]).astype(np.int32)
+    _run(b, idx, block=128)
+    b = _shared(Batch(45, [900], hq=8, hkv=4, page=32, e4m3=e4m3), 300, [1 + 3 * i for i in range(300)])
+    assert 300 * 4 * 512 * 256 > 96 << 20
+    _run(b, window=512)
+    b = _shared(Batch(46, [3000], hq=8, hkv=4, page=64, e4m3=e4m3), 3, [3000, 64, 1234])
+    b.table = np.concatenate([b.table, np.full((3, 1000), -1, dtype=np.int32)], 1)
+    _run(b)
+
+
+def test_random_calls():
+    """Sizes, layouts, selections and windows by lot."""
+    rng = np.random.default_rng(47)
+    for i in range(40):
+        hkv, g = int(rng.integers(1, 5)), int(rng.integers(1, 9))
+        n = int(rng.integers(1, 9))
+        kv = [int(rng.integers(0, 10 ** rng.integers(1, 4)) + 1) for _ in range(n)]
+        new = [min(k, int(rng.integers(0, 12))) for k in kv] if rng.random() < 0.5 else None
+        if new is not None and sum(new) == 0:
+            new[0] = 1
+        b = Batch(100 + i, kv, new, hq=hkv * g, hkv=hkv, page=int(rng.choice([16, 32, 64, 128, 256])), e4m3=bool(rng.random() < 0.5),
+                  pad=0 if new is None else int(rng.integers(0, 3)), before=0 if new is None else int(rng.integers(0, 3)))
+        block = int(rng.choice([64, 128]))
+        _run(b, b.draw_idx(int(rng.integers(1, 33)), block) if rng.random() < 0.5 else None, block, window=int(rng.choice([0, 0, 1, 50, 700])),
+             gate=bool(rng.random() < 0.3), acc=False, scale=float(rng.choice([0.0, 0.05])))
