@@ -111,6 +111,8 @@ class PagedCache:
         key = (tokens, nseq, hq, max_pages, block, topk, window, scale)
         known = self._shapes.get(key)
         if known is None:
+            if not (0 <= window < 2 ** 31 and 0 < block < 2 ** 31):
+                raise NsaSelError(f"window must be 0 or a number of tokens and block 64 or 128, got {window} and {block}")
             shape = CacheShape(tokens, nseq, hq, self.hkv, _D, self._dtype, self.page, self.n_pages, max_pages, block, topk, window, scale)
             need = C.c_size_t()
             _check(lib().nsa_sel_cache_workspace_bytes(C.byref(shape), C.byref(need)), "nsa_sel_cache_workspace_bytes")

@@ -337,8 +337,9 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
       if (r < rows_of(tile)) __builtin_nontemporal_store(to_e4m3(f[i], inverse), reinterpret_cast<uint64_t*>(to + r * kD));
     }
   };
-  // a head after the other; a page of one tile in one step, else its tiles twice: for the largest magnitude, and to be stored
-  const int its = tiles == 1 ? 1 : 2 * tiles;
+  // a head after the other; a page of one tile in one step, else its tiles twice: for the largest magnitude, and to be stored.  K_out is written
+  // in the last round: it may be K itself.
+  const int its = tiles == 1 || U.page < 0 ? tiles : 2 * tiles;
   u32x4 x[kSteps];
   float f[kSteps][8];
   load(0, h0, x);
@@ -353,7 +354,7 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
         if (tiles > 1) __syncthreads();  // the last tile's angles have been read
         angles(tile);
       }
-      amax = fmaxf(amax, turn(tile, h, it < tiles, x, f));
+      amax = fmaxf(amax, turn(tile, h, it + tiles >= its, x, f));
       const bool last = it + 1 == its;
       if (!last || h + 1 < h1) load(last ? 0 : it + 1 < tiles ? it + 1 : it + 1 - tiles, last ? h + 1 : h, x);
       if (U.page < 0) continue;  // the same for the whole workgroup

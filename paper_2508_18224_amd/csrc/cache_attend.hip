@@ -22,6 +22,7 @@ constexpr int kVRow = kD * 2;                 // bytes of a row of V in LDS, its
 constexpr int kSumRow = kD * 4 + 16;          // bytes of a column's sums in LDS
 constexpr int kOwnLds = (16 * kSumRow + 2 * 16 * 4 + 255) & ~255;  // a wavefront's: its tile of V, and later its sums and their statistics
 constexpr int kAttendLds = kWaves * kOwnLds;
+static_assert(kAttendLds <= 64 * 1024, "more would have to be asked for before the first launch");
 static_assert(kPiece * kVRow <= kOwnLds, "the tile of a wavefront must fit");
 static_assert(kTiles == 2, "a piece is one contraction step of the PV product");
 
@@ -618,7 +619,6 @@ hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, 
   const bool grouped = A.group > 1;
   const int64_t groups = grouped ? C.T / A.group + C.nseq : C.T;
   const int64_t grid = A.even > 0 ? A.even : groups * C.hkv * A.splits;
-  static std::atomic<uint64_t> ready[16];
   using Kernel = void (*)(Cache, CacheAttend);
 #define FORMS(e4m3, policy)                                                                                           \
   k_cache_attend<e4m3, true, false, policy>, k_cache_attend<e4m3, false, false, policy>,                              \
@@ -628,13 +628,11 @@ hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, 
 #undef FORMS
   const int form = (e4m3 ? 8 : 0) + (grouped ? (A.even > 0 ? 7 : 3) : (A.streaming ? 4 : 0) + (A.idx ? 0 : A.even > 0 ? 2 : 1));
   const Kernel kern = kForms[form];
-  hipError_t e = allow_dynamic_lds((const void*)kern, kAttendLds, ready[form]);
-  if (e != hipSuccess) return e;
   {
     ProfScope ps(KID_CACHE_ATTEND, st);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * kWaves), kAttendLds, st, C, A);
   }
-  e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.rows == nullptr) return e;
   ProfScope ps(KID_CACHE_JOIN, st);
   hipLaunchKernelGGL(k_cache_join, dim3((unsigned)((int64_t)C.T * C.hq)), dim3(256), 0, st, C, A);

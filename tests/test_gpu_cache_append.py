@@ -154,6 +154,26 @@ def test_in_place_and_far_places():
         _near(host(b.dk[t]), pco.rotate(b.k[t], 2 ** 20 + 74 + t, f, False), b.k[t], 2.0 ** -8)
 
 
+@pytest.mark.parametrize("page", [64, 256])
+def test_in_place_where_a_page_gets_more_than_the_mean(page):
+    """Few new tokens in the mean and many in one sequence: its page is gone through twice, and the keys may be their own results."""
+    new = [200] + [1] * 30
+    b = Batch(39, [210] + [7] * 30, new, hq=4, hkv=2, page=page, e4m3=True)
+    pages, scales = [x.copy() for x in b.pages], [x.copy() for x in b.scales]
+    f = _freq(128)
+    turned = pco.append(b.k, b.v, b.table, b.kv_len, b.cu, pages, scales, page, f, False)
+    cache = b.upload(nsa)
+    cache.append(b.dk, b.dv, b.dtable, b.dlen, b.dcu, q=b.dq, inv_freq=dev(f, torch.float64), q_out=b.dq, k_out=b.dk)
+    for t, (s, p) in enumerate(pco.places(b.kv_len, b.cu, b.T)):
+        _near(host(b.dk[t]), turned[t], b.k[t], 2.0 ** -8)
+        _near(host(b.dq[t]), pco.rotate(b.q[t], p, f, False), b.q[t], 2.0 ** -8)
+        at = pco.slot_of(b.table, b.n_pages, page, s, p)
+        unit = scales[0][at[0]][:, None]
+        _near(host(cache.k_pages[at[0], :, at[1]]), turned[t] / unit, b.k[t] / unit, 2.0 ** -4, 2.0 ** -10)
+        assert np.array_equal(host(cache.v_pages[at[0], :, at[1]]), pages[1][at[0], :, at[1]])
+    assert np.array_equal(host(cache.k_scale), scales[0]) and np.array_equal(host(cache.v_scale), scales[1])
+
+
 def test_without_queries_and_without_tokens():
     b = Batch(36, [9, 30], hq=2, hkv=2, page=16)
     cache = b.upload(nsa)

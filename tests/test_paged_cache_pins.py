@@ -176,7 +176,7 @@ def test_binding_refuses_wrong_tensors():
     idx, gate = z(3, 2, 4, dtype=i32), z(3, 8)
     for kw in (dict(q=q.float()), dict(q=q[0]), dict(q=z(3, 8, 256, dtype=bf)[..., ::2]), dict(idx=idx.long()), dict(idx=idx[:2]), dict(idx=idx[..., :0]),
                dict(gate=gate.double()), dict(o_acc=q), dict(gate=gate, o_acc=q.float()), dict(out=q.float()), dict(lse=gate.double()),
-               dict(cu=z(3, dtype=i32)), dict(ws=z(4)), dict(window=-1), dict(idx=idx, block=32), dict(idx=z(3, 2, 40, dtype=i32))):
+               dict(cu=z(3, dtype=i32)), dict(ws=z(4)), dict(window=-1), dict(window=2 ** 32 + 5), dict(idx=idx, block=2 ** 32 + 64), dict(idx=idx, block=32), dict(idx=z(3, 2, 40, dtype=i32))):
         with pytest.raises(E):
             cache.attention(**{**ok, **kw})
     x = z(3, 2, 8)
