@@ -259,7 +259,8 @@ int nsa_sel_cache_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* byte
  * With gate (DEVICE fp32 [n_tokens, hq]) O receives O_acc + gate * result instead, formed before the one rounding;
  * O_acc (bf16 like O, may be O itself) may be NULL for zero.  LSE is that of the attention either way.
  * A row without visible keys gets O = 0 (O_acc with a gate), LSE = -inf; so does one whose visible scores are all -inf.
- * Results are bit-reproducible and do not depend on the batch a token is in, but for the number of workgroups that share a row. */
+ * The same call gives the same bits; how a row's keys are shared among workgroups follows from the batch, so that a token's
+ * last bits may differ between batches. */
 int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, const int32_t* idx, const int32_t* cu_seqlens,
                             const int32_t* kv_len, const int32_t* table, const void* k_pages, const void* v_pages,
                             const float* k_scale, const float* v_scale, const float* gate, const void* O_acc, void* O,
