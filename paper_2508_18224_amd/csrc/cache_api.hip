@@ -70,7 +70,7 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   const int64_t each = s->nseq > 0 ? (s->n_tokens + (int64_t)s->nseq - 1) / s->nseq : 1;  // new tokens of a sequence, in the mean
   const int64_t most = 16 / g;
   c.group = s->topk > 0 ? 1 : (int)(each < most ? (each > 1 ? each : 1) : most);
-  const int64_t rows = (s->n_tokens + c.group - 1) / c.group * (int64_t)s->hkv;
+  const int64_t rows = ((int64_t)s->n_tokens + c.group - 1) / c.group * s->hkv;
   // upper bound of the pieces of a row (the kernel finds out how many there are, by the lengths and the kept blocks)
   const int64_t limit = (int64_t)s->max_pages * s->page, window = s->window;
   int64_t pieces = (limit + kAttendPiece - 1) / kAttendPiece;
@@ -96,7 +96,8 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   // Non-temporal loads where the keys and values are more than the 256 MB of the memory-side cache keep from one call to the next, and not for
   // new tokens of one sequence, which share blocks.  (16 blocks of 64, us, plain -> non-temporal: 256 tokens x 8 heads bf16, 1.05 GB, 188 -> 169; 32 x 8, 131 MB, 29.2
   // -> 26.0; 16 x 8, 66 MB, 17.1 -> 22.9; drafts of one to eight tokens, 524 MB read of half as much, 79 -> 94.)
-  const bool streaming = rows * pieces * kAttendPiece * kD * (s->dtype == NSA_SEL_CACHE_E4M3 ? 2 : 4) > (96ll << 20) && s->n_tokens == s->nseq;
+  const int64_t piece_bytes = (int64_t)kAttendPiece * kD * (s->dtype == NSA_SEL_CACHE_E4M3 ? 2 : 4);
+  const bool streaming = rows > (96ll << 20) / (pieces * piece_bytes) && s->n_tokens == s->nseq;
   if (chunk > pieces) chunk = pieces;
   c.chunk = (int)chunk;
   c.splits = (int)((pieces + chunk - 1) / chunk);

@@ -409,7 +409,7 @@ hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t
   const int each = (Q ? C.hq : 0) + (e4m3 ? 0 : 2 * C.hkv);
   auto rows = [&](auto kern, int tokens, int parts) {
     ProfScope ps(KID_CACHE_APPEND, st);
-    hipLaunchKernelGGL(kern, dim3((unsigned)((C.T + tokens - 1) / tokens), (unsigned)parts), dim3(kRowThreads), 0, st, C, A);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)C.T + tokens - 1) / tokens), (unsigned)parts), dim3(kRowThreads), 0, st, C, A);
     return hipGetLastError();
   };
   const bool many = C.T >= 4096;
@@ -426,7 +426,7 @@ hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t
   const bool apart = many && Q && (units * C.hkv >= 2048 || threads == 1024);
   const int64_t share = units * C.hkv / (threads == 64 ? 1024 : 512);
   const int heads = (int)std::min<int64_t>(std::max<int64_t>(share, 1), C.hkv), parts = many ? 1 : parts_of(threads / 16);
-  const int64_t row_groups = Q && !apart ? (many ? (C.T + 3) / 4 : (int64_t)C.T * parts) : 0;
+  const int64_t row_groups = Q && !apart ? (many ? ((int64_t)C.T + 3) / 4 : (int64_t)C.T * parts) : 0;
   const int64_t grid = 2 * units * ((C.hkv + heads - 1) / heads) + row_groups;
   const auto kern = !many            ? (threads == 64 ? k_cache_append_e4m3<64, 1> : k_cache_append_e4m3<256, 1>)
                     : row_groups > 0 ? (threads == 256 ? k_cache_append_e4m3<256, 4> : k_cache_append_e4m3<512, 4>)
