@@ -191,3 +191,44 @@ def test_pages_that_do_not_exist_are_not_written(e4m3):
     _run(b, 64, False)
     b.table = b.table[:, :6].copy()                                       # a table that ends before the length
     _run(b, 64, False)
+
+
+def test_random_appends():
+    """Sizes, layouts, places and rotations by lot."""
+    rng = np.random.default_rng(48)
+    for i in range(30):
+        hkv, g, n = int(rng.integers(1, 5)), int(rng.integers(1, 9)), int(rng.integers(1, 7))
+        kv = [int(rng.integers(0, 10 ** rng.integers(1, 4)) + 1) for _ in range(n)]
+        new = [min(k, int(rng.integers(0, 10 ** rng.integers(1, 3)))) for k in kv] if rng.random() < 0.6 else None
+        if new is not None and sum(new) == 0:
+            new[0] = 1
+        b = Batch(200 + i, kv, new, hq=hkv * g, hkv=hkv, page=int(rng.choice([16, 32, 64, 128, 256])), e4m3=bool(rng.random() < 0.6),
+                  pad=0 if new is None else int(rng.integers(0, 3)), before=0 if new is None else int(rng.integers(0, 3)))
+        _run(b, 16 * int(rng.integers(0, 9)), bool(rng.random() < 0.4), slices=bool(rng.random() < 0.3))
+
+
+@pytest.mark.parametrize("e4m3,page", [(False, 64), (True, 64), (True, 128), (True, 256)])
+def test_long_prompts(e4m3, page):
+    """From 4096 new tokens on rows and pages are gone through otherwise: heads share a page's angles, query rows are a launch of their own.  Against the
+    same tokens in calls of whole pages and fewer tokens, which are held to the oracle: bit for bit."""
+    rng = np.random.default_rng([49, page])
+    lens = [6000, 37, 2500]
+    hq, hkv, T = 12, 6, sum(lens)
+    q, k, v = (torch.randn(T, h, 128, device="cuda").bfloat16() for h in (hq, hkv, hkv))
+    per = -(-max(lens) // page)
+    table = dev(rng.permutation(3 * per).reshape(3, per), torch.int32)
+    f = dev(_freq(128, 500000.0), torch.float64)
+    one, many = (nsa.PagedCache(3 * per, hkv, page=page, dtype=E4M3 if e4m3 else torch.bfloat16) for _ in range(2))
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    qo, ko = one.append(k, v, table, dev(lens, torch.int32), dev(cu, torch.int32), q=q, inv_freq=f, rotated_k=True)
+    qs, ks = torch.empty_like(qo), torch.empty_like(ko)
+    for s, L in enumerate(lens):
+        for a in range(0, L, 1024):                        # whole pages a call
+            n = min(1024, L - a)
+            rows = slice(int(cu[s]) + a, int(cu[s]) + a + n)
+            many.append(k[rows], v[rows], table[s:s + 1], dev([a + n], torch.int32), dev([0, n], torch.int32), q=q[rows], inv_freq=f, q_out=qs[rows],
+                        k_out=ks[rows])
+    assert torch.equal(qo, qs) and torch.equal(ko, ks)
+    assert torch.equal(one.k_pages.view(torch.uint8), many.k_pages.view(torch.uint8)) and torch.equal(one.v_pages.view(torch.uint8), many.v_pages.view(torch.uint8))
+    if e4m3:
+        assert torch.equal(one.k_scale, many.k_scale) and torch.equal(one.v_scale, many.v_scale)
