@@ -71,6 +71,33 @@ def lib():
     return _lib
 
 
+_native = None
+
+
+def native():
+    """The compiled layer of the calls over a paged cache (csrc/bind_cache.cpp), beside the library."""
+    global _native
+    if _native is None:
+        lib()  # raises if the library has not been built
+        try:
+            from . import _cache_native
+        except ImportError as e:
+            raise NsaSelError(f"{e}: run `python -m paper_2508_18224_amd.build` first") from e
+        _cache_native.set_error(NsaSelError)
+        _native = _cache_native
+    return _native
+
+
+def call_native(fn, dev: torch.device, *args):
+    """fn(*args, current stream of dev) with dev current."""
+    if dev.type != "cuda":
+        return fn(*args, 0)  # refuses
+    if torch._C._cuda_getDevice() == dev.index:
+        return fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    with torch.cuda.device(dev):
+        return fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+
+
 def _check(rc: int, what: str):
     if rc != 0:
         raise NsaSelError(f"{what}: {lib().nsa_sel_strerror(rc).decode()} ({rc})")
@@ -230,30 +257,16 @@ def select_blocks(scores: torch.Tensor, cu: Optional[torch.Tensor], topk: int, *
     With kv_len (int32 [sequences], tokens of each cached sequence with its new ones) the rows are the new tokens of cached
     sequences (nsa_sel_select_blocks_cached, always causal): cu holds the starts of each sequence's new tokens, or is None for one
     new token each.  Rows of tokens that belong to no sequence are left as `out` has them, and are -1 in a new one."""
+    if kv_len is not None:
+        if not causal:
+            raise NsaSelError("new tokens of cached sequences are selected for causally")
+        if not isinstance(scores, torch.Tensor):
+            raise NsaSelError("scores must be a torch.Tensor")
+        return call_native((_native or native()).select_blocks, scores.device, scores, kv_len, cu, topk, block, n_sink, n_local, out)
     if scores.dtype != torch.float32 or scores.dim() != 3:
         raise NsaSelError("scores must be float32 [tokens, hkv, stride]")
     T, hkv, stride = scores.shape
     dev = scores.device
-    if kv_len is not None:
-        if not causal:
-            raise NsaSelError("new tokens of cached sequences are selected for causally")
-        nseq = kv_len.numel()
-        if cu is None and nseq != T:
-            raise NsaSelError(f"without cu_seqlens every sequence has one new token: {nseq} lengths for {T} tokens")
-        if out is not None:
-            expect_tensor("out", out, torch.int32, (T, hkv, topk), dev)
-        elif cu is None:
-            out = torch.empty((T, hkv, topk), dtype=torch.int32, device=dev)
-        else:
-            out = torch.full((T, hkv, topk), -1, dtype=torch.int32, device=dev)
-        if not scores.is_contiguous():
-            raise NsaSelError("scores must be contiguous")
-        expect_tensor("cu_seqlens", cu, torch.int32, (nseq + 1,), dev, optional=True)
-        expect_tensor("kv_len", kv_len, torch.int32, (nseq,), dev)
-        shape = CacheShape(T, nseq, hkv, hkv, 128, 0, 64, 0, 0, block, topk, 0, 0.0)
-        _launch(lib().nsa_sel_select_blocks_cached, "nsa_sel_select_blocks_cached", dev, C.byref(shape), _ptr(scores), stride, _ptr(cu),
-                _ptr(kv_len), n_sink, n_local, _ptr(out))
-        return out
     nseq = 1 if cu is None else cu.numel() - 1
     shape = Shape(T, nseq, hkv, hkv, 128, block, topk, int(causal), 0.0, 0)
     if out is None:
