@@ -205,7 +205,7 @@ int nsa_sel_select_blocks(const nsa_sel_shape* shape, const float* scores, int64
  *   - table is int32 [nseq, max_pages]: column c of row s names the page that holds the places [c * page, (c + 1) * page)
  *     of sequence s.  Entries outside [0, n_pages), and columns past max_pages, are no pages: nothing is written to them
  *     and their keys are invisible.  Sequences may share pages that none of them is appending to.
- *   - kv_len is int32 [nseq]: tokens of each sequence INCLUDING the new ones.  The new tokens of all sequences are packed
+ *   - kv_len is int32 [nseq]: tokens of each sequence INCLUDING the new ones, at most 2^30.  The new tokens of all sequences are packed
  *     like a training batch: cu_seqlens int32 [nseq + 1] holds their starts; NULL means one new token for each sequence
  *     (n_tokens == nseq).  New token i of n of sequence s has place kv_len[s] - n + i; tokens of negative place are not
  *     appended and see nothing.  Tokens before cu_seqlens[0] and from cu_seqlens[nseq] on belong to no sequence: their rows

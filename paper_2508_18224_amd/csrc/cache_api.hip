@@ -57,6 +57,9 @@ int check_cache_pointers(const nsa_sel_cache_shape* s, const void* k, const void
   return NSA_SEL_OK;
 }
 
+// No place is as far back as 2^30 of another: a window that long is none, and the kernels' sums with one stay in 32 bits.
+int32_t window_of(const nsa_sel_cache_shape* s) { return s->window < (1 << 30) ? s->window : 0; }
+
 // How the attention is cut (see launch_cache_attend).
 struct Cut {
   int group;           // new tokens of a sequence that a workgroup takes together
@@ -72,7 +75,7 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   c.group = s->topk > 0 ? 1 : (int)(each < most ? (each > 1 ? each : 1) : most);
   const int64_t rows = ((int64_t)s->n_tokens + c.group - 1) / c.group * s->hkv;
   // upper bound of the pieces of a row (the kernel finds out how many there are, by the lengths and the kept blocks)
-  const int64_t limit = (int64_t)s->max_pages * s->page, window = s->window;
+  const int64_t limit = (int64_t)s->max_pages * s->page, window = window_of(s);
   int64_t pieces = (limit + kAttendPiece - 1) / kAttendPiece;
   if (s->topk > 0) {
     int64_t blocks = (limit + s->block - 1) / s->block;
@@ -180,7 +183,7 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
   A.idx = idx;
   A.block = shape->topk > 0 ? shape->block : kBlock;
   A.topk = shape->topk;
-  A.window = shape->window;
+  A.window = window_of(shape);
   A.scale = shape->scale > 0.f ? shape->scale : 0.08838834764831845f;  // 1/sqrt(128)
   A.gate = gate;
   A.o_acc = O_acc;

@@ -176,6 +176,17 @@ def test_every_key_cut_evenly(kv, new, hq, hkv, page, window, e4m3):
     _run(b, window=window, gate=True)
 
 
+@pytest.mark.parametrize("new", [None, [3, 9]])
+def test_windows_longer_than_any_sequence(new):
+    """They hide nothing, up to the longest that the argument holds; rows cut evenly, whole rows, selected blocks."""
+    for kv in ([3000, 200], [300, 5]):  # of the latter's new tokens some have a negative place
+        b = Batch(70 + kv[0], kv, new, hq=8, hkv=2, page=64)
+        idx = b.draw_idx(4, 64)
+        for window in (3001, 2 ** 30 - 1, 2 ** 30, 2 ** 31 - 16, 2 ** 31 - 1):
+            _run(b, window=window)
+            _run(b, idx, window=window)
+
+
 def test_more_sequences_than_are_cut_evenly():
     """Every sequence is a workgroup's where a scan over the batch would cost more than it gives; a long table all the same."""
     b = Batch(41, [i % 50 for i in range(4100)] , hq=2, hkv=1, page=16)
