@@ -79,6 +79,20 @@ float number(PyObject* o) {
   return (float)v;
 }
 
+// Other Python threads run while torch allocates and the library launches: the allocator may wait, and so may a full queue.
+struct WithoutGil {
+  PyThreadState* state = PyEval_SaveThread();
+  ~WithoutGil() { PyEval_RestoreThread(state); }
+};
+template <class F>
+auto without_gil(F&& f) {
+  const WithoutGil w;
+  return f();
+}
+at::Tensor empty(at::IntArrayRef shape, at::TensorOptions options) {
+  return without_gil([&] { return at::empty(shape, options); });
+}
+
 void done(int rc, const char* what) {
   if (rc != NSA_SEL_OK) throw Refused{std::string(what) + ": " + nsa_sel_strerror(rc) + " (" + std::to_string(rc) + ")"};
 }
@@ -211,7 +225,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (a[10] != Py_None) {
         q_out = expect(tensor(a[10], "q_out"), "q_out", at::kBFloat16, rows, c.device);
       } else {
-        new_q = at::empty(rows, options);
+        new_q = empty(rows, options);
         q_out = new_q.data_ptr();
       }
     } else if (a[10] != Py_None) {
@@ -220,7 +234,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[11] != Py_None) {
       k_out = expect(tensor(a[11], "k_out"), "k_out", at::kBFloat16, kv_rows, c.device);
     } else if (truth(a[9])) {
-      new_k = at::empty(kv_rows, options);
+      new_k = empty(kv_rows, options);
       k_out = new_k.data_ptr();
     }
     const double* freq = nullptr;
@@ -233,8 +247,12 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const nsa_sel_cache_shape s = shape_of(c, b, T, hq);
     on_gpu(c.device);
-    done(nsa_sel_cache_append(&s, q_ptr, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, b.cu, b.kv_len, b.table, freq, (int32_t)(2 * pairs),
-                              truth(a[8]), c.k, c.v, c.ks, c.vs, q_out, k_out, PyLong_AsVoidPtr(a[12])),
+    const bool interleaved = truth(a[8]);
+    void* const stream = PyLong_AsVoidPtr(a[12]);
+    done(without_gil([&] {
+           return nsa_sel_cache_append(&s, q_ptr, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, b.cu, b.kv_len, b.table, freq,
+                                       (int32_t)(2 * pairs), interleaved, c.k, c.v, c.ks, c.vs, q_out, k_out, stream);
+         }),
          "nsa_sel_cache_append");
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
@@ -289,24 +307,26 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (w.nbytes() < need) throw Refused{"ws holds " + std::to_string(w.nbytes()) + " bytes, " + std::to_string(need) + " are needed"};
       ws = w.data_ptr();
     } else if (need > 0) {
-      new_ws = at::empty({(int64_t)need}, options.dtype(at::kByte));
+      new_ws = empty({(int64_t)need}, options.dtype(at::kByte));
       ws = new_ws.data_ptr();
     }
     if (a[11] != Py_None) {
       out = expect(tensor(a[11], "out"), "out", at::kBFloat16, rows, c.device);
     } else {
-      new_o = at::empty(rows, options.dtype(at::kBFloat16));
+      new_o = empty(rows, options.dtype(at::kBFloat16));
       out = new_o.data_ptr();
     }
     if (a[12] != Py_None) {
       lse = expect(tensor(a[12], "lse"), "lse", at::kFloat, per_row, c.device);
     } else {
-      new_l = at::empty(per_row, options.dtype(at::kFloat));
+      new_l = empty(per_row, options.dtype(at::kFloat));
       lse = new_l.data_ptr();
     }
     on_gpu(c.device);
-    done(nsa_sel_cache_attention(&s, q_ptr, idx, b.cu, b.kv_len, b.table, c.k, c.v, c.ks, c.vs, gate, acc, out, (float*)lse, ws, need,
-                                 PyLong_AsVoidPtr(a[14])),
+    void* const stream = PyLong_AsVoidPtr(a[14]);
+    done(without_gil([&] {
+           return nsa_sel_cache_attention(&s, q_ptr, idx, b.cu, b.kv_len, b.table, c.k, c.v, c.ks, c.vs, gate, acc, out, (float*)lse, ws, need, stream);
+         }),
          "nsa_sel_cache_attention");
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
@@ -350,12 +370,15 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
       out = expect(tensor(a[7], "out"), "out", at::kInt, rows, dev);
     } else {
       const auto options = at::TensorOptions().dtype(at::kInt).device(dev);
-      made = cu ? at::full(rows, -1, options) : at::empty(rows, options);  // rows of no sequence stay -1
+      made = cu ? without_gil([&] { return at::full(rows, -1, options); }) : empty(rows, options);  // rows of no sequence stay -1
       out = made.data_ptr();
     }
     on_gpu(dev);
-    done(nsa_sel_select_blocks_cached(&s, (const float*)scores, stride, cu, (const int32_t*)kv_len, small(a[5], "n_sink"), small(a[6], "n_local"),
-                                      (int32_t*)out, PyLong_AsVoidPtr(a[8])),
+    const int32_t n_sink = small(a[5], "n_sink"), n_local = small(a[6], "n_local");
+    void* const queue = PyLong_AsVoidPtr(a[8]);
+    done(without_gil([&] {
+           return nsa_sel_select_blocks_cached(&s, (const float*)scores, stride, cu, (const int32_t*)kv_len, n_sink, n_local, (int32_t*)out, queue);
+         }),
          "nsa_sel_select_blocks_cached");
     return made.defined() ? THPVariable_Wrap(std::move(made)) : given(a[7]);
   } catch (const Refused& r) {

@@ -185,3 +185,43 @@ def test_calls_go_to_the_current_stream():
     assert not s.query()
     s.synchronize()
     assert torch.equal(o, want)
+
+
+def test_calls_of_several_threads():
+    """Threads with a stream each make all three calls at once, into caches of their own; each gets what it gets alone."""
+    import threading
+    batches = [Batch(63 + i, [900 - 100 * i, 70 + i, 300], hq=HQ, hkv=HKV, page=64, e4m3=i % 2 == 1) for i in range(4)]
+    freq = dev(10000.0 ** (-np.arange(0, 128, 2) / 128), torch.float64)
+    scores = [torch.rand(b.T, HKV, 16, device="cuda") for b in batches]
+
+    def step(b, x):
+        q, k = b.cache.append(b.dk, b.dv, b.dtable, b.dlen, q=b.dq, inv_freq=freq, rotated_k=True)
+        idx = nsa.select_blocks(x, None, TOPK, kv_len=b.dlen)
+        return (q, k, idx, *b.cache.attention(q, b.dtable, b.dlen, idx=idx), *b.cache.attention(q, b.dtable, b.dlen))
+
+    want = []
+    for b, x in zip(batches, scores):
+        b.upload(nsa)
+        step(b, x)  # appended again, a page's scale has grown already
+        want.append([y.clone() for y in step(b, x)])
+    got, failed = [None] * 4, []
+    torch.cuda.synchronize()
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for _ in range(50):
+                    got[i] = step(batches[i], scores[i])
+            s.synchronize()
+        except Exception as e:  # shown by the assertion below
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, w))
