@@ -2,7 +2,7 @@
 //
 // One pass over the keys with the running maximum and sum of a softmax.  What bounds it is reading the keys and values, which nothing else
 // reads: 4 g flops a byte in bf16 and twice that in 8 bits, far below what the matrix cores need to be busy.  So the products may waste
-// most of their columns (g of 16 are in use for a token), and everything serves having bytes in flight: a wavefront takes pieces of 32
+// most of their columns (of 16 a token uses g, twice: see where its probabilities are split), and everything serves having bytes in flight: a wavefront takes pieces of 32
 // keys by itself, K straight into the registers that the product reads, V through registers into a tile of its own in LDS, and the next
 // piece is requested as soon as the registers are free.  The wavefronts of a workgroup take pieces in turn and join their sums in LDS; where
 // there are too few rows to fill the chip several workgroups share one, and a second kernel joins theirs.
@@ -146,9 +146,9 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
   part.begin = __builtin_amdgcn_readfirstlane(part.begin);
   part.end = __builtin_amdgcn_readfirstlane(part.end);
   const int limit = C.max_pages << C.page_log2;  // places that the table can name
-  // this lane's column: token tt of the group, head hh; it sees the places [c_lo, c_hi)
-  const int tt = kGroup ? col / C.g : 0, hh = col - tt * C.g, cols = W.nt * C.g;
-  const bool used = col < cols;
+  // this lane's column: token tt of the group, head hh; it sees the places [c_lo, c_hi).  Without groups column c + 8 is c's again.
+  const int own_col = kGroup ? col : col & 7, tt = kGroup ? col / C.g : 0, hh = own_col - tt * C.g, cols = W.nt * C.g;
+  const bool used = own_col < cols;
   // what any column sees, and what all of them see
   const int lo = A.window > 0 ? max(W.place + 1 - A.window, 0) : 0, hi = min(W.place + W.nt, limit);
   const int all_lo = A.window > 0 ? max(W.place + W.nt - A.window, 0) : 0, all_hi = min(W.place + 1, limit);
@@ -320,15 +320,21 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
     const float mc = m_new == -INFINITY ? 0.f : m_new * c2;
     const float alpha = __builtin_amdgcn_exp2f(fmaf(m_run, c2, -mc));  // exp2(-inf) = 0 on the first piece with a score
     m_run = m_new;
+    // A probability goes into the product in two parts, the bf16 value below it and the rest as bf16, so that its first 16 bits count: as one bf16
+    // value it would lose up to 2^-8 of itself, and sums of values that cancel four times what the rounding of O does.  The rest is never zero, as zero
+    // times an infinite value would be NaN.  Without groups the columns from 8 on, which repeat the others, have it; a group's may all be in use, and
+    // it is a product of its own.
     float l = 0.f;
-    bf16x8 pf;
+    bf16x8 pf, pr;
 #pragma unroll
     for (int x = 0; x < kTiles; ++x)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float p = __builtin_amdgcn_exp2f(fmaf(sacc[x][e], c2, -mc));
         l += p;
-        pf[4 * x + e] = (bf16_t)p;
+        const float high = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) & 0xffff0000u), rest = fmaxf(p - high, 0x1p-126f);
+        pf[4 * x + e] = (bf16_t)(kGroup || col < 8 ? high : rest);
+        if constexpr (kGroup) pr[4 * x + e] = (bf16_t)rest;
       }
     l_run = fmaf(l_run, alpha, l);
 #pragma unroll
@@ -357,7 +363,11 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
     wave_sync();
     if (!kGroup || (cur.key0 >= all_lo && cur.key0 + kPiece <= all_hi)) {
 #pragma unroll
-      for (int d = 0; d < 8; ++d) oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values(va, d), pf, oacc[d], 0, 0, 0);
+      for (int d = 0; d < 8; ++d) {
+        const bf16x8 a = values(va, d);
+        oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf, oacc[d], 0, 0, 0);
+        if constexpr (kGroup) oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pr, oacc[d], 0, 0, 0);
+      }
     } else {
       // Tokens of the group see different keys of the piece, and what one does not see may be an infinity or a NaN, which a
       // probability of zero does not silence: one token at a time, the others' keys as zeros.
@@ -371,7 +381,8 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
             const int key = 16 * (e >> 2) + 4 * qg + (e & 3);
             if (key < k_lo || key >= k_hi) a[e] = (bf16_t)0.f;
           }
-          const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pr, add, 0, 0, 0);
           if (tt == k) oacc[d] += add;
         }
       }
@@ -408,7 +419,11 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
     const float* ml = reinterpret_cast<const float*>(from + 16 * kSumRow);
     const float f = __builtin_amdgcn_exp2f(fmaf(ml[c], c2, -tc));
     total = fmaf(f, ml[16 + c], total);
-    const f32x4 a = *reinterpret_cast<const f32x4*>(from + c * kSumRow + 32 * sub), b = *reinterpret_cast<const f32x4*>(from + c * kSumRow + 32 * sub + 16);
+    f32x4 a = *reinterpret_cast<const f32x4*>(from + c * kSumRow + 32 * sub), b = *reinterpret_cast<const f32x4*>(from + c * kSumRow + 32 * sub + 16);
+    if constexpr (!kGroup) {
+      a += *reinterpret_cast<const f32x4*>(from + (c + 8) * kSumRow + 32 * sub);
+      b += *reinterpret_cast<const f32x4*>(from + (c + 8) * kSumRow + 32 * sub + 16);
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       o[e] = fmaf(f, a[e], o[e]);
