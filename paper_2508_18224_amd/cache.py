@@ -26,7 +26,10 @@ class PagedCache:
         o, lse = cache.attention(q, table, kv_len, idx=idx)
 
     Forward only.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
-    race, as writes to any tensor do."""
+    race, as writes to any tensor do.
+
+    k_pages, v_pages, k_scale, v_scale (None in bfloat16), n_pages, hkv, page and device are there to be read.  The tensors are looked at in every call:
+    their owner may give them other storage in between, of the same shape.  A larger cache is another PagedCache."""
 
     def __init__(self, n_pages: int, hkv: int, *, page: int = 64, dtype: torch.dtype = _BF16, device="cuda:0"):
         device = _device(device)
@@ -50,9 +53,18 @@ class PagedCache:
     def _set(self, k_pages, v_pages, k_scale, v_scale):
         self._calls = native()
         self._info = self._calls.describe(k_pages, v_pages, k_scale, v_scale)
-        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
-        self.n_pages, self.hkv, self.page, _ = k_pages.shape
-        self.device = k_pages.device
+        self._tensors = (k_pages, v_pages, k_scale, v_scale)
+        self._sizes = tuple(k_pages.shape[:3])
+        self._device = k_pages.device
+
+    k_pages = property(lambda self: self._tensors[0])
+    v_pages = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
+    n_pages = property(lambda self: self._sizes[0])
+    hkv = property(lambda self: self._sizes[1])
+    page = property(lambda self: self._sizes[2])
+    device = property(lambda self: self._device)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
                q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
@@ -64,7 +76,7 @@ class PagedCache:
         channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved.  rotated_k also returns the rotated keys, for the prompt's own
         attention.  q_out / k_out take the results (they may be q / k themselves if those are contiguous); rows of tokens that belong to no
         sequence are left as they are there, and uninitialised otherwise."""
-        return call_native(self._calls.append, self.device, self._info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out)
+        return call_native(self._calls.append, self._device, self._info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out)
 
     def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
         """Bytes that attention() of such a call needs as `ws`."""
@@ -83,4 +95,4 @@ class PagedCache:
 
         out / lse take the results (out may be o_acc); rows of tokens that belong to no sequence are left as they are there, and
         uninitialised otherwise.  ws, of workspace_bytes(), is for callers that may not allocate."""
-        return call_native(self._calls.attention, self.device, self._info, q, table, kv_len, cu, idx, block, window, scale, gate, o_acc, out, lse, ws)
+        return call_native(self._calls.attention, self._device, self._info, q, table, kv_len, cu, idx, block, window, scale, gate, o_acc, out, lse, ws)

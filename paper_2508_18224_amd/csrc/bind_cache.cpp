@@ -103,11 +103,10 @@ void count(Py_ssize_t got, Py_ssize_t want) {
   if (got != want) throw Refused{"internal: wrong number of arguments"};
 }
 
-// ---- a cache: its pages' addresses and sizes ----------------------------------------------------------------------------------
+// ---- a cache: its tensors and sizes ----------------------------------------------------------------------------------------------
 struct CacheInfo {
-  at::Tensor keep[4];
-  void *k, *v;
-  float *ks, *vs;
+  at::Tensor t[4];  // K and V pages and, in 8 bits, their scales
+  at::ScalarType type;
   int32_t n_pages, hkv, page, dtype;
   at::Device device = at::kCPU;
 };
@@ -117,6 +116,28 @@ const CacheInfo& info(PyObject* o) {
   auto* p = static_cast<CacheInfo*>(PyCapsule_GetPointer(o, kCapsule));
   if (!p) throw python_error();
   return *p;
+}
+
+// Where they lie at this call: their owner may have given them other storage since the last one, or none.
+struct Pages {
+  void *k, *v;
+  float *ks = nullptr, *vs = nullptr;
+};
+void* address(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape, const at::Device& dev) {
+  if (t.has_storage() && t.storage().nbytes() < (size_t)(t.storage_offset() + t.numel()) * t.itemsize()) throw Refused{std::string(name) + " has lost its storage"};
+  return expect(t, name, type, shape, dev);
+}
+Pages pages(const CacheInfo& c) {
+  const int64_t shape[4] = {c.n_pages, c.hkv, c.page, kD};
+  const at::IntArrayRef scales(shape, 2);
+  Pages p;
+  p.k = address(c.t[0], "k_pages", c.type, shape, c.device);
+  p.v = address(c.t[1], "v_pages", c.type, shape, c.device);
+  if (c.dtype == NSA_SEL_CACHE_E4M3) {
+    p.ks = (float*)address(c.t[2], "k_scale", at::kFloat, scales, c.device);
+    p.vs = (float*)address(c.t[3], "v_scale", at::kFloat, scales, c.device);
+  }
+  return p;
 }
 
 PyObject* describe(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -132,23 +153,20 @@ PyObject* describe(PyObject*, PyObject* const* a, Py_ssize_t n) {
       throw Refused{"pages must be [n_pages, hkv, page, 128] with 16, 32, 64, 128 or 256 tokens a page, got " + text(s)};
     auto c = std::make_unique<CacheInfo>();
     c->device = k.device();
+    c->type = type;
     c->n_pages = (int32_t)s[0];
     c->hkv = (int32_t)s[1];
     c->page = (int32_t)p;
     c->dtype = type == at::kBFloat16 ? NSA_SEL_CACHE_BF16 : NSA_SEL_CACHE_E4M3;
-    c->k = expect(k, "k_pages", type, s, c->device);
-    c->v = expect(dims(a[1], "v_pages", 4), "v_pages", type, s, c->device);
-    c->ks = c->vs = nullptr;
-    c->keep[0] = k;
-    c->keep[1] = THPVariable_Unpack(a[1]);
+    c->t[0] = k;
+    c->t[1] = dims(a[1], "v_pages", 4);
     if (c->dtype == NSA_SEL_CACHE_E4M3) {
-      c->ks = (float*)expect(dims(a[2], "k_scale", 2), "k_scale", at::kFloat, {s[0], s[1]}, c->device);
-      c->vs = (float*)expect(dims(a[3], "v_scale", 2), "v_scale", at::kFloat, {s[0], s[1]}, c->device);
-      c->keep[2] = THPVariable_Unpack(a[2]);
-      c->keep[3] = THPVariable_Unpack(a[3]);
+      c->t[2] = dims(a[2], "k_scale", 2);
+      c->t[3] = dims(a[3], "v_scale", 2);
     } else if (a[2] != Py_None || a[3] != Py_None) {
       throw Refused{"bfloat16 pages have no scales"};
     }
+    pages(*c);
     PyObject* o = PyCapsule_New(c.get(), kCapsule, free_info);
     if (o) c.release();
     return o;
@@ -207,6 +225,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   try {
     count(n, 13);
     const CacheInfo& c = info(a[0]);
+    const Pages p = pages(c);
     const at::Tensor &k = dims(a[1], "k", 3), &v = dims(a[2], "v", 3);
     const int64_t T = k.size(0);
     const int64_t kv_rows[3] = {T, c.hkv, kD};
@@ -251,7 +270,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* const stream = PyLong_AsVoidPtr(a[12]);
     done(without_gil([&] {
            return nsa_sel_cache_append(&s, q_ptr, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, b.cu, b.kv_len, b.table, freq,
-                                       (int32_t)(2 * pairs), interleaved, c.k, c.v, c.ks, c.vs, q_out, k_out, stream);
+                                       (int32_t)(2 * pairs), interleaved, p.k, p.v, p.ks, p.vs, q_out, k_out, stream);
          }),
          "nsa_sel_cache_append");
     PyObject* r = PyTuple_New(2);
@@ -272,6 +291,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   try {
     count(n, 15);
     const CacheInfo& c = info(a[0]);
+    const Pages p = pages(c);
     const at::Tensor& q = dims(a[1], "q", 3);
     const int64_t T = q.size(0), hq = q.size(1);
     const int64_t rows[3] = {T, hq, kD}, per_row[2] = {T, hq};
@@ -325,7 +345,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     on_gpu(c.device);
     void* const stream = PyLong_AsVoidPtr(a[14]);
     done(without_gil([&] {
-           return nsa_sel_cache_attention(&s, q_ptr, idx, b.cu, b.kv_len, b.table, c.k, c.v, c.ks, c.vs, gate, acc, out, (float*)lse, ws, need, stream);
+           return nsa_sel_cache_attention(&s, q_ptr, idx, b.cu, b.kv_len, b.table, p.k, p.v, p.ks, p.vs, gate, acc, out, (float*)lse, ws, need, stream);
          }),
          "nsa_sel_cache_attention");
     PyObject* r = PyTuple_New(2);
