@@ -25,7 +25,7 @@ class PagedCache:
         idx = select_blocks(scores, None, topk, kv_len=kv_len)
         o, lse = cache.attention(q, table, kv_len, idx=idx)
 
-    Forward only.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
+    Forward only: in grad mode tensors that require grad are refused.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
     race, as writes to any tensor do.
 
     k_pages, v_pages, k_scale, v_scale (None in bfloat16), n_pages, hkv, page and device are there to be read.  The tensors are looked at in every call:

@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -41,6 +42,8 @@ void expect_kind(const at::Tensor& t, const char* name, at::ScalarType type, at:
   if (t.scalar_type() != type) throw Refused{std::string(name) + " must be " + c10::toString(type) + ", got " + c10::toString(t.scalar_type())};
   if (t.sizes() != shape) throw Refused{std::string(name) + " must have shape " + text(shape) + ", got " + text(t.sizes())};
   if (t.device() != dev) throw Refused{std::string(name) + " must live on " + dev.str() + ", got " + t.device().str()};
+  if (t.requires_grad() && at::GradMode::is_enabled())
+    throw Refused{std::string(name) + " requires grad, and the calls over a cache have no backward: call under torch.no_grad(), or detach it"};
 }
 // A contiguous tensor; its address.
 void* expect(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape, const at::Device& dev) {
@@ -368,7 +371,7 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = dims(a[0], "scores", 3);
     const at::Device dev = x.device();
     const int64_t T = x.size(0), hkv = x.size(1), stride = x.size(2);
-    const void* scores = expect(x, "scores", at::kFloat, x.sizes(), dev);
+    const void* scores = expect(x.requires_grad() ? x.detach() : x, "scores", at::kFloat, x.sizes(), dev);  // block ids have no gradient
     const at::Tensor& lengths = dims(a[1], "kv_len", 1);
     const int64_t nseq = lengths.size(0);
     if (T > INT32_MAX || hkv > INT32_MAX || nseq > INT32_MAX) throw Refused{"too many tokens, heads or sequences"};

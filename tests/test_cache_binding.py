@@ -54,3 +54,27 @@ def test_tensors_that_became_others_are_refused(which):
         for call in _calls(cache):
             with pytest.raises(nsa.NsaSelError, match=NAMES[which]):
                 call()
+
+
+def test_gradients_are_refused_not_lost():
+    """Neither call has a backward: in grad mode a tensor that requires grad is refused, by its name; without grad mode it is a tensor like others."""
+    bf, i32 = torch.bfloat16, torch.int32
+    q, k, f = torch.zeros(3, 8, 128, dtype=bf), torch.zeros(3, 2, 128, dtype=bf), torch.zeros(64, dtype=torch.float64)
+    gate, lse = torch.zeros(3, 8), torch.zeros(3, 8)
+    table, kv_len = torch.zeros(3, 4, dtype=i32), torch.ones(3, dtype=i32)
+    cache = nsa.PagedCache(5, 2, device="cpu")
+    append = dict(k=k, v=k.clone(), q=q, inv_freq=f, q_out=q.clone(), k_out=k.clone())
+    attention = dict(q=q, gate=gate, o_acc=q.clone(), out=q.clone(), lse=lse)
+    for call, args in ((cache.append, append), (cache.attention, attention)):
+        for name in args:
+            mine = {**args, name: args[name].clone().requires_grad_()}
+            with pytest.raises(nsa.NsaSelError, match=f"^{name} requires grad"):
+                call(table=table, kv_len=kv_len, **mine)
+            with torch.no_grad(), pytest.raises(nsa.NsaSelError, match="device tensors"):  # all that is wrong here
+                call(table=table, kv_len=kv_len, **mine)
+    cache.k_pages.requires_grad_()
+    for call, args in ((cache.append, append), (cache.attention, attention)):
+        with pytest.raises(nsa.NsaSelError, match="^k_pages requires grad"):
+            call(table=table, kv_len=kv_len, **args)
+    with pytest.raises(nsa.NsaSelError, match="device tensors"):                              # ids have no gradient to lose
+        nsa.select_blocks(torch.zeros(3, 2, 8, requires_grad=True), None, 4, kv_len=kv_len)
