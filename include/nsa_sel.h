@@ -210,7 +210,9 @@ int nsa_sel_select_blocks(const nsa_sel_shape* shape, const float* scores, int64
  *     (n_tokens == nseq).  New token i of n of sequence s has place kv_len[s] - n + i; tokens of negative place are not
  *     appended and see nothing.  Tokens before cu_seqlens[0] and from cu_seqlens[nseq] on belong to no sequence: their rows
  *     of every output are left as they were.  Sequences may have no new token.
- *   - What lies in a page behind a sequence's last token is never looked at, whatever it holds. */
+ *   - What lies in a page behind a sequence's last token is never looked at, whatever it holds.
+ *   - A call whose launch would have 2^32 work-items or more is EUNSUPPORTED, before anything is launched: 2^24 new tokens in an append to bf16 pages, as many
+ *     tokens times KV heads in an attention over selected blocks.  nsa_sel_cache_workspace_bytes says so for an attention. */
 #define NSA_SEL_CACHE_BF16 0
 #define NSA_SEL_CACHE_E4M3 1
 

@@ -17,7 +17,12 @@ struct Cache {
   int32_t T, nseq, hq, hkv, g, n_pages, max_pages, page_log2;
 };
 
-hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+// HIP takes no launch of 2^32 work-items or more along a grid's dimension.
+constexpr bool launchable(int64_t workgroups, int threads) { return workgroups <= (((int64_t)1 << 32) - 1) / threads; }
+constexpr int kAttendThreads = 256, kJoinThreads = 256;
+
+// Returns a status of the C ABI.
+int launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
                                const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, void* Q_out,
                                void* K_out, hipStream_t st);
 
@@ -41,6 +46,7 @@ struct CacheAttend {
   float2* part_ml;     // [slots, cols] (maximum, sum)
   int4* rows;          // [T, hkv] first slot, second slot, number of parts, first token of the row
   int32_t slots, cols, slot_step;
+  int32_t workgroups;
 };
 hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, hipStream_t st);
 

@@ -9,7 +9,7 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 bool tensor(const void* p, bool or_null = false) { return p ? aligned(p, 16) : or_null; }
 bool ints(const void* p, bool or_null = false) { return p ? aligned(p, 4) : or_null; }
 
-int check_cache_shape(const nsa_sel_cache_shape* s, bool attention) {
+int check_sizes(const nsa_sel_cache_shape* s, bool attention) {
   if (!s) return NSA_SEL_EINVAL;
   if (s->n_tokens < 0 || s->nseq < 0 || (s->nseq == 0 && s->n_tokens > 0) || s->hq < 1 || s->hkv < 1 || s->n_pages < 0 || s->max_pages < 0)
     return NSA_SEL_EINVAL;
@@ -66,6 +66,7 @@ struct Cut {
   int splits, chunk, even;
   bool streaming;
   int64_t slots;       // of parts; 0 where every row is one workgroup's
+  int64_t workgroups;
 };
 Cut cut_of(const nsa_sel_cache_shape* s) {
   Cut c;
@@ -95,7 +96,9 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   // Every key: rows of up to 40 pieces, and many rows of a window, are a workgroup each; longer ones are cut evenly (see k_cache_attend_even).
   // (8 heads, us, whole -> even: 16 sequences of 1024 14.9 -> 19.1, one of 2048 22 -> 10.2, a window of 512 x 128 sequences 12.3 -> 41, of 4096 x 64 170
   // either way.)
-  const bool even = s->topk == 0 && pieces > 40 && s->nseq <= 4096 && !(window > 0 && rows >= 512);
+  // Not where there are too many rows for the launch that joins parts: whole ones fill the chip as well then.
+  const int64_t joins = (int64_t)s->n_tokens * s->hq;
+  const bool even = s->topk == 0 && pieces > 40 && s->nseq <= 4096 && !(window > 0 && rows >= 512) && launchable(joins, kJoinThreads);
   // Non-temporal loads where the keys and values are more than the 256 MB of the memory-side cache keep from one call to the next, and not for
   // new tokens of one sequence, which share blocks.  (16 blocks of 64, us, plain -> non-temporal: 256 tokens x 8 heads bf16, 1.05 GB, 188 -> 169; 32 x 8, 131 MB, 29.2
   // -> 26.0; 16 x 8, 66 MB, 17.1 -> 22.9; drafts of one to eight tokens, 524 MB read of half as much, 79 -> 94.)
@@ -107,8 +110,14 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   c.even = even ? 512 : 0;
   if (c.even && rows > (((int64_t)1 << 31) - 1) / pieces * c.even) c.even = 0;  // a share is a 32-bit number
   c.streaming = streaming;
-  c.slots = c.even ? 2 * (int64_t)c.even : c.splits > 1 ? rows * c.splits : 0;
+  c.slots = c.even ? 2 * (int64_t)c.even : c.splits > 1 ? rows * c.splits : 0;  // (parts of selected blocks: of fewer than 512 rows)
+  const int64_t groups = c.group > 1 ? s->n_tokens / c.group + (int64_t)s->nseq : s->n_tokens;
+  c.workgroups = c.even ? c.even : groups * s->hkv * c.splits;
   return c;
+}
+int check_cache_shape(const nsa_sel_cache_shape* s, bool attention) {
+  const int rc = check_sizes(s, attention);
+  return rc == NSA_SEL_OK && attention && !launchable(cut_of(s).workgroups, kAttendThreads) ? NSA_SEL_EUNSUPPORTED : rc;
 }
 struct CacheWs {
   size_t ml, rows, total;  // offsets; the sums come first
@@ -149,9 +158,7 @@ int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_
   if (2 * units * shape->hkv + shape->n_tokens >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;  // workgroups
   const Cache C = make_cache(shape, k_pages, v_pages, k_scale, v_scale, table, kv_len, cu_seqlens);
   return launch_cache_append(C, shape->dtype == NSA_SEL_CACHE_E4M3, Q, q_stride, K, k_stride, V, v_stride, inv_freq, rot,
-                             interleaved != 0, Q_out, K_out, (hipStream_t)stream) == hipSuccess
-             ? NSA_SEL_OK
-             : NSA_SEL_EHIP;
+                             interleaved != 0, Q_out, K_out, (hipStream_t)stream);
 }
 
 int nsa_sel_cache_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes) {
@@ -176,8 +183,6 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
   const CacheWs w = cache_ws(shape, c);
   if (w.total > 0 && !tensor(ws)) return NSA_SEL_EINVAL;
   if (ws_bytes < w.total) return NSA_SEL_EWORKSPACE;
-  const int64_t groups = c.group > 1 ? shape->n_tokens / c.group + (int64_t)shape->nseq : shape->n_tokens;
-  if (groups * shape->hkv * c.splits >= ((int64_t)1 << 31) || c.slots >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;  // workgroups
   CacheAttend A;
   A.Q = Q;
   A.idx = idx;
@@ -200,6 +205,7 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
   A.cols = c.group * (shape->hq / shape->hkv);
   A.slots = (int)c.slots;
   A.slot_step = c.even ? 2 : 1;
+  A.workgroups = (int)c.workgroups;
   const Cache C = make_cache(shape, k_pages, v_pages, k_scale, v_scale, table, kv_len, cu_seqlens);
   return launch_cache_attend(C, shape->dtype == NSA_SEL_CACHE_E4M3, A, (hipStream_t)stream) == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP;
 }

@@ -391,9 +391,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 64 ? 3 : 4) k_cache_appe
 
 }  // namespace
 
-hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
-                               const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, void* Q_out,
-                               void* K_out, hipStream_t st) {
+int launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                        const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, void* Q_out,
+                        void* K_out, hipStream_t st) {
   AppendArgs A;
   A.Q = (const bf16_t*)Q;
   A.K = (const bf16_t*)K;
@@ -407,10 +407,13 @@ hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t
   A.R.rot = rot;
   A.R.interleaved = interleaved ? 1 : 0;
   const int each = (Q ? C.hq : 0) + (e4m3 ? 0 : 2 * C.hkv);
+  auto status = [] { return hipGetLastError() == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP; };
+  auto groups = [&](int tokens) { return ((int64_t)C.T + tokens - 1) / tokens; };
   auto rows = [&](auto kern, int tokens, int parts) {
+    if (!launchable(groups(tokens), kRowThreads)) return NSA_SEL_EUNSUPPORTED;
     ProfScope ps(KID_CACHE_APPEND, st);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)C.T + tokens - 1) / tokens), (unsigned)parts), dim3(kRowThreads), 0, st, C, A);
-    return hipGetLastError();
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups(tokens), (unsigned)parts), dim3(kRowThreads), 0, st, C, A);
+    return status();
   };
   const bool many = C.T >= 4096;
   // a token's rows over as many as 512 workgroups
@@ -431,16 +434,13 @@ hipError_t launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t
   const auto kern = !many            ? (threads == 64 ? k_cache_append_e4m3<64, 1> : k_cache_append_e4m3<256, 1>)
                     : row_groups > 0 ? (threads == 256 ? k_cache_append_e4m3<256, 4> : k_cache_append_e4m3<512, 4>)
                                      : (threads == 256 ? k_cache_append_e4m3<256, 0> : threads == 512 ? k_cache_append_e4m3<512, 0> : k_cache_append_e4m3<1024, 0>);
+  if (!launchable(grid, threads) || (apart && !launchable(groups(4), kRowThreads))) return NSA_SEL_EUNSUPPORTED;
   {
     ProfScope ps(KID_CACHE_APPEND, st);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(threads), 0, st, C, A, (int)units, heads, parts);
   }
-  if (apart) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    return rows(k_cache_append_rows<4, false>, 4, 1);
-  }
-  return hipGetLastError();
+  const int rc = status();
+  return rc == NSA_SEL_OK && apart ? rows(k_cache_append_rows<4, false>, 4, 1) : rc;
 }
 
 }  // namespace nsa

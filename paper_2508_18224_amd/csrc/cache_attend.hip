@@ -27,6 +27,7 @@ constexpr int kOwnLds = (16 * kSumRow + 2 * 16 * 4 + 255) & ~255;  // a wavefron
 constexpr int kAttendLds = kWaves * kOwnLds;
 static_assert(kAttendLds <= 64 * 1024, "more would have to be asked for before the first launch");
 static_assert(kPiece * kVRow <= kOwnLds, "the tile of a wavefront must fit");
+static_assert(64 * kWaves == kAttendThreads, "the host reckons with this many");
 static_assert(kTiles == 2, "a piece is one contraction step of the PV product");
 
 __device__ __forceinline__ void wave_sync() {
@@ -570,7 +571,7 @@ __global__ void __launch_bounds__(64 * kWaves, kGroup ? 2 : 3) k_cache_attend_ev
 }
 
 // The parts of a row: a workgroup a row, whose groups of 16 lanes, 8 channels a lane, take them in turn.
-__global__ void __launch_bounds__(256) k_cache_join(Cache C, CacheAttend A) {
+__global__ void __launch_bounds__(kJoinThreads) k_cache_join(Cache C, CacheAttend A) {
   __shared__ float sums[16][kD + 4], stats[16];
   const int64_t row = blockIdx.x;
   const int t = (int)(row / C.hq), h = (int)(row - (int64_t)t * C.hq), grp = threadIdx.x >> 4, sub = threadIdx.x & 15;
@@ -635,8 +636,6 @@ __global__ void __launch_bounds__(256) k_cache_join(Cache C, CacheAttend A) {
 
 hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, hipStream_t st) {
   const bool grouped = A.group > 1;
-  const int64_t groups = grouped ? C.T / A.group + C.nseq : C.T;
-  const int64_t grid = A.even > 0 ? A.even : groups * C.hkv * A.splits;
   using Kernel = void (*)(Cache, CacheAttend);
 #define FORMS(e4m3, policy)                                                                                           \
   k_cache_attend<e4m3, true, false, policy>, k_cache_attend<e4m3, false, false, policy>,                              \
@@ -648,12 +647,12 @@ hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, 
   const Kernel kern = kForms[form];
   {
     ProfScope ps(KID_CACHE_ATTEND, st);
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * kWaves), kAttendLds, st, C, A);
+    hipLaunchKernelGGL(kern, dim3((unsigned)A.workgroups), dim3(kAttendThreads), kAttendLds, st, C, A);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.rows == nullptr) return e;
   ProfScope ps(KID_CACHE_JOIN, st);
-  hipLaunchKernelGGL(k_cache_join, dim3((unsigned)((int64_t)C.T * C.hq)), dim3(256), 0, st, C, A);
+  hipLaunchKernelGGL(k_cache_join, dim3((unsigned)((int64_t)C.T * C.hq)), dim3(kJoinThreads), 0, st, C, A);
   return hipGetLastError();
 }
 

@@ -399,7 +399,7 @@ int launch_select(const float* scores, int64_t score_stride, const int32_t* cu, 
   const bool many = !kv_len && eight_rows(rows, hkv);
   const int64_t per = many ? kSelRows : 1;
   const int64_t grid = (rows + kSelWaves * per - 1) / (kSelWaves * per);
-  if (grid >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
+  if (!launchable(grid, 64 * kSelWaves)) return NSA_SEL_EUNSUPPORTED;
   ProfScope prof(KID_SELECT_BLOCKS, st);
   const bool vec = (score_stride & 3) == 0 && ((uintptr_t)scores & 15) == 0;
   auto kern = kv_len ? (vec ? k_select_blocks<true, false, true> : k_select_blocks<false, false, true>)
