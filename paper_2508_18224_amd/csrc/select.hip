@@ -391,10 +391,10 @@ int launch_select(const float* scores, int64_t score_stride, const int32_t* cu, 
   if (topk < 1 || topk > kMaxTopk) return NSA_SEL_EUNSUPPORTED;
   if (!scores) score_stride = (int64_t)kMaxChunks * kChunkBlocks;   // no rows to stay inside
   if (score_stride < 1 || score_stride > (int64_t)kMaxChunks * kChunkBlocks) return NSA_SEL_EUNSUPPORTED;
+  const int64_t rows = (int64_t)T * hkv;
+  if (rows == 0) return NSA_SEL_OK;  // an empty tensor may have no address
   if (!idx || ((uintptr_t)scores & 3) || ((uintptr_t)idx & 3)) return NSA_SEL_EINVAL;   // scores may be NULL
   if (!cu && nseq != (kv_len ? T : 1)) return NSA_SEL_EINVAL;
-  const int64_t rows = (int64_t)T * hkv;
-  if (rows == 0) return NSA_SEL_OK;
   if (rows * topk >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
   const bool many = !kv_len && eight_rows(rows, hkv);
   const int64_t per = many ? kSelRows : 1;
