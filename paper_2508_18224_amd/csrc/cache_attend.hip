@@ -441,9 +441,10 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
     if (sub == 0) A.part_ml[at] = float2{top, total};
     return;
   }
-  const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
+  const bool some = total > 0.f || total != total;
+  const float inv = 1.f / total;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] *= inv;
+  for (int e = 0; e < 8; ++e) o[e] = some ? o[e] * inv : 0.f;  // an empty row is 0 whatever its values are
   if (A.gate) {
     const float gate = A.gate[row];
     u32x4 x = u32x4{0u, 0u, 0u, 0u};
@@ -458,7 +459,7 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
   *reinterpret_cast<u32x4*>((bf16_t*)A.O + row * kD + 8 * sub) = x;
-  if (sub == 0) A.LSE[row] = total > 0.f || total != total ? (tc + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+  if (sub == 0) A.LSE[row] = some ? (tc + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
 }
 
 // A row a workgroup, or with A.splits the `chunk` pieces of a row that are its own.
@@ -619,9 +620,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(Cache C, CacheAtten
     total += stats[g];
   }
   const bool some = total > 0.f || total != total;
-  const float inv = some ? 1.f / total : 0.f;
-  p *= inv;
-  q *= inv;
+  const float inv = 1.f / total;
+  p = some ? p * inv : 0.f;
+  q = some ? q * inv : 0.f;
   if (A.gate) {
     const float gate = A.gate[row];
     const uint32_t x = A.o_acc ? reinterpret_cast<const uint32_t*>(A.o_acc)[row * (kD / 2) + lane] : 0u;

@@ -65,3 +65,24 @@ def test_infinite_values_that_are_seen(kv, new, selected):
     assert np.isposinf(ref[..., 5]).any() and np.isneginf(ref[..., 70]).any() and np.isnan(ref[..., 9]).any()
     for f in (np.isposinf, np.isneginf, np.isnan):
         assert np.array_equal(f(o), f(ref))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("kv,new", [([70], None), ([3000], None), ([70, 20], [3, 5])])
+def test_an_empty_row_is_zero_whatever_its_values_are(kv, new, e4m3):
+    """Every visible score is -inf: O = 0 (o_acc with a gate) and LSE = -inf, with values that are infinite or NaN too."""
+    b = Batch(9 + sum(kv), kv, new, hq=4, hkv=1, page=64, e4m3=e4m3)
+    b.q = pco.to_bf16(np.abs(b.q) + 0.25)
+    if e4m3:                                              # no infinite key; a score of -inf comes from the query
+        b.q[..., 5] = np.inf
+        b.pages[0][..., 5] = np.where(np.isnan(b.pages[0][..., 5]), np.nan, -1.0)
+    else:
+        b.pages[0][..., 5] = np.where(np.isnan(b.pages[0][..., 5]), np.nan, -np.inf)
+    b.pages[1][..., 9] = np.nan
+    b.pages[1][..., 64] = np.nan if e4m3 else np.inf
+    cache = b.upload(nsa)
+    o, lse = cache.attention(b.dq, b.dtable, b.dlen, b.dcu)
+    assert (o == 0).all() and torch.isneginf(lse).all()
+    acc = torch.randn(b.T, 4, 128, device="cuda").bfloat16()
+    o, lse = cache.attention(b.dq, b.dtable, b.dlen, b.dcu, gate=torch.rand(b.T, 4, device="cuda"), o_acc=acc)
+    assert torch.equal(o, acc) and torch.isneginf(lse).all()
