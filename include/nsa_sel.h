@@ -242,7 +242,8 @@ typedef struct {
  *   K itself if k_stride = hkv * d).
  * bf16: one rounding of the rotated value.  e4m3: the scale of a (page, head) is the least 2^e with |x| <= 448 * 2^e for all
  * new values x of the call in that page; in a page that held earlier tokens of the sequence it never shrinks, and where it
- * grows they are rounded again to the new scale (exact except for values below 2^-14 of it).  Values then are rounded to the
+ * grows they are rounded again to the new scale (exact except for values below 2^-6 of it, each of which is off by 2^-10 of it
+ * at most).  Values then are rounded to the
  * nearest; infinities and NaN are stored as NaN and do not count for the scale, and what the largest scale cannot hold is
  * stored as 448 * 2^119.  A page's other slots are left as they are.  Pages that are written must not be named twice in
  * the call. */
