@@ -207,8 +207,9 @@ int nsa_sel_select_blocks(const nsa_sel_shape* shape, const float* scores, int64
  *     and their keys are invisible.  Sequences may share pages that none of them is appending to.
  *   - kv_len is int32 [nseq]: tokens of each sequence INCLUDING the new ones, at most 2^30.  The new tokens of all sequences are packed
  *     like a training batch: cu_seqlens int32 [nseq + 1] holds their starts; NULL means one new token for each sequence
- *     (n_tokens == nseq).  New token i of n of sequence s has place kv_len[s] - n + i; tokens of negative place are not
- *     appended and see nothing.  Tokens before cu_seqlens[0] and from cu_seqlens[nseq] on belong to no sequence: their rows
+ *     (n_tokens == nseq).  New token i of n of sequence s has place kv_len[s] - n + i; tokens of negative place (an idle slot
+ *     of a padded batch, with kv_len[s] = 0) are not appended, their rows of Q_out and K_out are left as they were, and they
+ *     see nothing, whatever their query holds: O = 0, LSE = -inf, idx = -1.  Tokens before cu_seqlens[0] and from cu_seqlens[nseq] on belong to no sequence: their rows
  *     of every output are left as they were.  Sequences may have no new token.
  *   - What lies in a page behind a sequence's last token is never looked at, whatever it holds.
  *   - A call whose launch would have 2^32 work-items or more is EUNSUPPORTED, before anything is launched: 2^24 new tokens in an append to bf16 pages, as many

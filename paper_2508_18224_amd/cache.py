@@ -75,7 +75,8 @@ class PagedCache:
         inv_freq: float64 [rot / 2], radians per place, rot a multiple of 16 up to 128 leading channels; None rotates nothing.  Pairs are
         channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved.  rotated_k also returns the rotated keys, for the prompt's own
         attention.  q_out / k_out take the results (they may be q / k themselves if those are contiguous); rows of tokens that belong to no
-        sequence are left as they are there, and uninitialised otherwise."""
+        sequence, and of tokens of negative place (idle slots, with kv_len 0), are left as they are there, and uninitialised otherwise: attention looks at
+        neither."""
         return call_native(self._calls.append, self._device, self._info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out)
 
     def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
