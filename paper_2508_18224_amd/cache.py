@@ -81,6 +81,9 @@ class PagedCache:
 
     def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
         """Bytes that attention() of such a call needs as `ws`."""
+        for name, x in dict(tokens=tokens, hq=hq, nseq=nseq, max_pages=max_pages, topk=topk, block=block, window=window).items():
+            if not -2 ** 31 <= x < 2 ** 31:
+                raise NsaSelError(f"{name} is out of range")
         shape = CacheShape(tokens, nseq, hq, self.hkv, _D, int(self.k_pages.dtype is not _BF16), self.page, self.n_pages, max_pages, block, topk, window, 0.0)
         need = C.c_size_t()
         _check(lib().nsa_sel_cache_workspace_bytes(C.byref(shape), C.byref(need)), "nsa_sel_cache_workspace_bytes")

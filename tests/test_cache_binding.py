@@ -78,3 +78,14 @@ def test_gradients_are_refused_not_lost():
             call(table=table, kv_len=kv_len, **args)
     with pytest.raises(nsa.NsaSelError, match="device tensors"):                              # ids have no gradient to lose
         nsa.select_blocks(torch.zeros(3, 2, 8, requires_grad=True), None, 4, kv_len=kv_len)
+
+
+def test_workspace_sizes_of_numbers_that_are_too_large():
+    """They would be taken modulo 2^32: the size of another call."""
+    cache = nsa.PagedCache(5, 2, device="cpu")
+    ok = dict(tokens=3, hq=8, nseq=3, max_pages=4000, topk=0, block=64, window=0)
+    assert cache.workspace_bytes(**ok) > 0
+    for name in ok:
+        for far in (2 ** 32, -2 ** 32, 2 ** 31):
+            with pytest.raises(nsa.NsaSelError, match=f"^{name} is out of range"):
+                cache.workspace_bytes(**{**ok, name: ok[name] + far if far != 2 ** 31 else far})
