@@ -104,7 +104,6 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   // -> 26.0; 16 x 8, 66 MB, 17.1 -> 22.9; drafts of one to eight tokens, 524 MB read of half as much, 79 -> 94.)
   const int64_t piece_bytes = (int64_t)kAttendPiece * kD * (s->dtype == NSA_SEL_CACHE_E4M3 ? 2 : 4);
   const bool streaming = rows > (96ll << 20) / (pieces * piece_bytes) && s->n_tokens == s->nseq;
-  if (chunk > pieces) chunk = pieces;
   c.chunk = (int)chunk;
   c.splits = (int)((pieces + chunk - 1) / chunk);
   c.even = even ? 512 : 0;
