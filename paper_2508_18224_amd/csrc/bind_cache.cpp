@@ -1,6 +1,6 @@
 // The Python calls over a paged cache (cache.py, select_blocks of binding.py) down to the C ABI: checks of the tensors, outputs and workspace, one call.
 // A decoding loop makes these calls a few times a layer with a few tokens, and what a call costs on the host is then what it costs: with the checks
-// in Python an append of one token took 10.1 us, its attention 14.7 and its selection 8.4, of which a launch is 3.7; from here 5.7, 10.4 and 5.4.
+// in Python an append of one token took 10.1 us, its attention 14.7 and its selection 8.4, of which a launch is 3.7; from here 5.6, 10.3 and 5.2.
 // The library knows nothing of this file or of torch.
 #include <Python.h>
 

@@ -75,7 +75,9 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   const int64_t most = 16 / g;
   c.group = s->topk > 0 ? 1 : (int)(each < most ? (each > 1 ? each : 1) : most);
   const int64_t rows = ((int64_t)s->n_tokens + c.group - 1) / c.group * s->hkv;
-  // upper bound of the pieces of a row (the kernel finds out how many there are, by the lengths and the kept blocks)
+  // Upper bound of the pieces of a row (the kernel finds out how many there are, by the lengths and the kept blocks).  Lengths are the device's: without a
+  // selection or a window all the host has is the table's width, and the rules below were measured on tables that fit their sequences.  Where the table is much
+  // wider, short sequences are cut as long ones are (16 of 1024 in a table of 131072 places 14.6 -> 17.0 us, two of 4096 12.9 -> 13.5).
   const int64_t limit = (int64_t)s->max_pages * s->page, window = window_of(s);
   int64_t pieces = (limit + kAttendPiece - 1) / kAttendPiece;
   if (s->topk > 0) {
@@ -88,20 +90,19 @@ Cut cut_of(const nsa_sel_cache_shape* s) {
   }
   if (pieces < 1) pieces = 1;
   // Selected blocks: a row is one workgroup's, unless there are so few rows that those would read at the rate of a few compute units: then
-  // about 512 workgroups, of a piece a wavefront at least.  (16 blocks of 64, bf16, us, whole -> in parts of 4 pieces: 1 token x 8 heads 14.4 -> 9.8,
-  // 4 x 8 15.6 -> 12.4, 16 x 8 17.1 -> 21.8 (of 8: 19.2); 32 blocks of 128, 1 x 2 45 -> 11.2.)
+  // about 512 workgroups, of a piece a wavefront at least.  (16 blocks of 64, bf16, us, whole -> in parts of 4 pieces: 1 token x 8 heads 14.4 -> 9.7,
+  // 4 x 8 15.5 -> 12.2, 16 x 8 16.9 -> 21.8 (of 8: 18.9); 32 blocks of 128, 1 x 2 44 -> 11.3.)
   int64_t chunk = (pieces * rows + 511) / 512;
   if (chunk < 4) chunk = 4;
   if (s->topk == 0 || 2 * chunk > pieces || (rows > 64 && pieces <= 64)) chunk = pieces;
   // Every key: rows of up to 40 pieces, and many rows of a window, are a workgroup each; longer ones are cut evenly (see k_cache_attend_even).
-  // (8 heads, us, whole -> even: 16 sequences of 1024 14.9 -> 19.1, one of 2048 22 -> 10.2, a window of 512 x 128 sequences 12.3 -> 41, of 4096 x 64 170
-  // either way.)
-  // Not where there are too many rows for the launch that joins parts: whole ones fill the chip as well then.
+  // (8 heads, bf16, us, whole -> even: 16 sequences of 1024 15.3 -> 19.1, one of 2048 22.0 -> 10.1, a window of 4096 x 64 sequences 170 -> 174; of 512 x 128, 4 heads,
+  // e4m3, 13.2 -> 43.)  Not where there are too many rows for the launch that joins parts: whole ones fill the chip as well then.
   const int64_t joins = (int64_t)s->n_tokens * s->hq;
   const bool even = s->topk == 0 && pieces > 40 && s->nseq <= 4096 && !(window > 0 && rows >= 512) && launchable(joins, kJoinThreads);
   // Non-temporal loads where the keys and values are more than the 256 MB of the memory-side cache keep from one call to the next, and not for
-  // new tokens of one sequence, which share blocks.  (16 blocks of 64, us, plain -> non-temporal: 256 tokens x 8 heads bf16, 1.05 GB, 188 -> 169; 32 x 8, 131 MB, 29.2
-  // -> 26.0; 16 x 8, 66 MB, 17.1 -> 22.9; drafts of one to eight tokens, 524 MB read of half as much, 79 -> 94.)
+  // new tokens of one sequence, which share blocks.  (16 blocks of 64, us, plain -> non-temporal: 256 tokens x 8 heads bf16, 1.05 GB, 183 -> 169; 32 x 8, 131 MB, 28.4
+  // -> 25.8; 16 x 8, 66 MB, 16.9 -> 23.3; drafts of one to eight tokens, 524 MB read of half as much, 79 -> 94.)
   const int64_t piece_bytes = (int64_t)kAttendPiece * kD * (s->dtype == NSA_SEL_CACHE_E4M3 ? 2 : 4);
   const bool streaming = rows > (96ll << 20) / (pieces * piece_bytes) && s->n_tokens == s->nseq;
   c.chunk = (int)chunk;

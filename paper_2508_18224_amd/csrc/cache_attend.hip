@@ -2,7 +2,7 @@
 //
 // One pass over the keys with the running maximum and sum of a softmax.  What bounds it is reading the keys and values, which nothing else
 // reads: 4 g flops a byte in bf16 and twice that in 8 bits, far below what the matrix cores need to be busy.  So the products may waste
-// most of their columns (of 16 a token uses g, twice: see where its probabilities are split), and everything serves having bytes in flight: a wavefront takes pieces of 32
+// columns (of 16 a token uses g, and as many again for the rest of its probabilities), and everything serves having bytes in flight: a wavefront takes pieces of 32
 // keys by itself, K straight into the registers that the product reads, V through registers into a tile of its own in LDS, and the next
 // piece is requested as soon as the registers are free.  The wavefronts of a workgroup take pieces in turn and join their sums in LDS; where
 // there are too few rows to fill the chip several workgroups share one, and a second kernel joins theirs.
@@ -10,8 +10,8 @@
 // S^T = K Q^T by 16x16x32 products: a lane holds four consecutive keys of one column, and the keys of two 16-key tiles are eight
 // consecutive contraction steps of O^T += V^T P^T if V's rows are read in the same order.  Nothing is transposed but V, by the LDS read.
 //
-// Measured: 256 tokens x 8 heads x 16 blocks of 64, bf16, 1.05 GB in 159 us, 6.6 TB/s; 8 sequences of 4096 .. 131072 tokens, g = 8, e4m3, every key,
-// 0.67 GB in 111 us with the join, 6.0 TB/s; one token, 16 blocks, 6.8 us and 3.2 for the join.
+// Measured: 256 tokens x 8 heads x 16 blocks of 64, bf16, 1.05 GB in 158 us, 6.6 TB/s; 8 sequences of 4096 .. 131072 tokens, g = 8, e4m3, every key,
+// 0.67 GB in 111 us with the join, 6.0 TB/s; one token, 16 blocks, 6.9 us and 3.6 for the join.
 //
 // e4m3 values become bf16 in registers, times their page's power of two, which bf16 holds exactly: the products are those of a bf16 cache.
 #include "cache.h"
