@@ -322,8 +322,8 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
     const float alpha = __builtin_amdgcn_exp2f(fmaf(m_run, c2, -mc));  // exp2(-inf) = 0 on the first piece with a score
     m_run = m_new;
     // A probability goes into the product in two parts, the bf16 value below it and the rest as bf16, so that its first 16 bits count: as one bf16
-    // value it would lose up to 2^-8 of itself, and sums of values that cancel four times what the rounding of O does.  The rest is never zero, as zero
-    // times an infinite value would be NaN.  Without groups the columns from 8 on, which repeat the others, have it; a group's may all be in use, and
+    // value it would lose up to 2^-8 of itself, and sums of values that cancel up to five times what the rounding of O does.  The rest is zero only where the
+    // probability is: zero times an infinite value would be NaN.  Without groups the columns from 8 on, which repeat the others, have it; a group's may all be in use, and
     // it is a product of its own.
     float l = 0.f;
     bf16x8 pf, pr;
@@ -333,7 +333,7 @@ __device__ __forceinline__ void attend(const Cache& C, const CacheAttend& A, Row
       for (int e = 0; e < 4; ++e) {
         const float p = __builtin_amdgcn_exp2f(fmaf(sacc[x][e], c2, -mc));
         l += p;
-        const float high = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) & 0xffff0000u), rest = fmaxf(p - high, 0x1p-126f);
+        const float high = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) & 0xffff0000u), rest = fmaxf(p - high, fminf(p, 0x1p-126f));
         pf[4 * x + e] = (bf16_t)(kGroup || col < 8 ? high : rest);
         if constexpr (kGroup) pr[4 * x + e] = (bf16_t)rest;
       }

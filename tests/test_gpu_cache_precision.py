@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2508_18224_amd as nsa
-from cache_util import Batch, dev, host
+from cache_util import Batch, check_attention, dev, host
 from oracle import paged_cache_oracle as pco
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +86,25 @@ def test_an_empty_row_is_zero_whatever_its_values_are(kv, new, e4m3):
     acc = torch.randn(b.T, 4, 128, device="cuda").bfloat16()
     o, lse = cache.attention(b.dq, b.dtable, b.dlen, b.dcu, gate=torch.rand(b.T, 4, device="cuda"), o_acc=acc)
     assert torch.equal(o, acc) and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("kv,new", [([200], None), ([3000], None), ([200, 90], [3, 5])])
+def test_large_values_without_weight(kv, new):
+    """A key whose score is -inf, or far below the others, weighs nothing, with the largest finite value too."""
+    b = Batch(11 + sum(kv), kv, new, hq=8, hkv=2, page=64)
+    b.q = pco.to_bf16(np.abs(b.q) + 0.25)
+    most = float(torch.finfo(torch.bfloat16).max)
+    for s in range(len(kv)):
+        for u, k, at in ((3, -np.inf, 5), (17, -np.inf, 5), (21, -1e20, 7), (40, -1e20, 64)):
+            p = b.table[s, u // 64]
+            b.pages[0][p, :, u % 64, at], b.pages[1][p, :, u % 64] = k, most * (-1) ** u
+    for k in (3, 17, 21, 40):
+        assert k < min(kv) - 8
+    finite = [np.where(np.isinf(b.pages[0]), 0.0, b.pages[0]), b.pages[1]]
+    with np.errstate(invalid="ignore"):
+        O, LSE, A, S = pco.attend(b.q, b.table, b.kv_len, b.cu, b.pages, b.scales, 64)
+    clean = [np.where(np.abs(x) > 1e19, 0.0, x) for x in finite]
+    S = pco.attend(b.q, b.table, b.kv_len, b.cu, clean, b.scales, 64)[3]
+    assert np.abs(O).max() < 100 and A.max() < 100        # those values are not in them
+    o, lse = b.upload(nsa).attention(b.dq, b.dtable, b.dlen, b.dcu)
+    check_attention(o, lse, (O, LSE, A, S))
