@@ -270,6 +270,25 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
                             const float* k_scale, const float* v_scale, const float* gate, const void* O_acc, void* O,
                             float* LSE, void* ws, size_t ws_bytes, void* stream);
 
+/* Bytes of the workspace of nsa_sel_cache_attention_chunk for `shape`. */
+int nsa_sel_cache_chunk_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes);
+
+/* nsa_sel_cache_attention for pieces of prompts: the same result (topk must be 0: every key, or a window) for many new tokens of a sequence, which share what they read of it:
+ * up to 256 / g tokens at a time, where the call above shares among 16 / g.  Right for any number of new tokens, made for 16 and more.  A probability is rounded to
+ * bf16 for its product with the values, as in nsa_sel_fwd, where the call above gives it 16 bits.
+ * The same call gives the same bits; how the keys are shared among workgroups follows from the batch, so that a token's last bits may differ between batches. */
+int nsa_sel_cache_attention_chunk(const nsa_sel_cache_shape* shape, const void* Q, const int32_t* cu_seqlens, const int32_t* kv_len,
+                                  const int32_t* table, const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
+                                  const float* gate, const void* O_acc, void* O, float* LSE, void* ws, size_t ws_bytes, void* stream);
+
+/* Reads keys and values back: rows K and V [n_tokens, hkv, d] bf16, with k_stride, v_stride elements between tokens (multiples of 8, at least hkv * d), of the places that
+ * an append of n_tokens new tokens with the same cu_seqlens and kv_len would write (new token i of n: kv_len - n + i; to read a whole sequence, n = kv_len).  What
+ * is stored in e4m3 stands for value * scale, which bf16 holds exactly.  Rows whose place is negative or has no page are zero; rows of no
+ * sequence are left as they were.  Uses shape->n_tokens, nseq, hkv, dtype, page, n_pages and max_pages; hq must be a valid number of query heads (hkv will do). */
+int nsa_sel_cache_read(const nsa_sel_cache_shape* shape, const int32_t* cu_seqlens, const int32_t* kv_len, const int32_t* table,
+                       const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, void* K, int64_t k_stride,
+                       void* V, int64_t v_stride, void* stream);
+
 /* nsa_sel_select_blocks for the new tokens of cached sequences: the same rule, causal, with the token's place in its
  * sequence taken from kv_len (cur = place / block, visible blocks 0 .. cur; a negative place sees none).  scores is DEVICE
  * fp32 [n_tokens, hkv, score_stride] or NULL, idx DEVICE int32 [n_tokens, hkv, topk].  Blocks from score_stride on do not
@@ -277,6 +296,31 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
 int nsa_sel_select_blocks_cached(const nsa_sel_cache_shape* shape, const float* scores, int64_t score_stride,
                                  const int32_t* cu_seqlens, const int32_t* kv_len, int32_t n_sink, int32_t n_local,
                                  int32_t* idx, void* stream);
+
+/* ---- rotary positions ------------------------------------------------------------------------------------------------
+ * Queries and keys of a packed batch turned by their places, as nsa_sel_cache_append turns them on the way to a cache (with factor 1 bit for bit), for the
+ * training path: Q_out, K_out [n_tokens, heads, d] bf16 from Q, K.  Pair i of a row at place p, channels a and b, becomes
+ * factor * (x_a cos - x_b sin), factor * (x_b cos + x_a sin) of the angle p * inv_freq[i]; the channels from rot on are copied.  The gradient of this
+ * is the same call with inverse != 0 on the gradients of the results.
+ *   positions int32 [n_tokens] (DEVICE) gives every token's place, of either sign; NULL: its place in its sequence by cu_seqlens, which may be NULL for one sequence
+ *   and is not looked at beside positions.  Tokens of no sequence (before cu_seqlens[0], from cu_seqlens[nseq] on) are copied as they are.
+ *   inv_freq is DEVICE double [rot / 2], radians per place; angles are formed in 64 bits.  Contexts longer than a model was made for change inv_freq and factor.
+ *   q_stride .. k_out_stride are elements between tokens, multiples of 8, at least heads * d; the heads of a token are contiguous.  K and K_out are NULL with
+ *   hkv = 0.  A result may be its own input with the same stride; other overlaps are not allowed. */
+typedef struct {
+  int32_t n_tokens;       /* rows of Q and K; >= 0                                                                */
+  int32_t nseq;           /* packed sequences, >= 1 unless positions are given                                    */
+  int32_t hq, hkv;        /* heads of Q (>= 1) and K (>= 0), any numbers; hq + hkv <= 65536                       */
+  int32_t d;              /* head dimension; 128 only                                                             */
+  int32_t rot;            /* leading channels that turn: a multiple of 16 up to d, 0 for none                     */
+  int32_t interleaved;    /* 0: pairs (i, i + rot / 2); else (2 i, 2 i + 1)                                       */
+  int32_t inverse;        /* != 0: by the negative angle                                                          */
+  double  factor;         /* of the turned channels; <= 0 selects 1                                               */
+} nsa_sel_rotary_shape;
+
+int nsa_sel_rotary(const nsa_sel_rotary_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                   const int32_t* cu_seqlens, const int32_t* positions, const double* inv_freq, void* Q_out, int64_t q_out_stride,
+                   void* K_out, int64_t k_out_stride, void* stream);
 
 /* Optional per-kernel timing for benchmarks (not part of the paper's method).  After
  * nsa_sel_profile_enable(capacity > 0) every kernel launch of the calls above is bracketed by a pair of HIP

@@ -8,3 +8,4 @@ from .binding import (NsaSelError, Shape, build_index, index_view, lib, native, 
                       workspace_bytes, workspace_bytes_min, SelAttention, select_blocks, window_blocks, profile_enable, profile_select, profile_collect, calibration_copy, mfma_probe, SYMBOLS)
 from .autograd import selected_attention  # noqa: F401,E402
 from .cache import PagedCache  # noqa: F401,E402
+from .rotary import rotary, rotary_frequencies  # noqa: F401,E402

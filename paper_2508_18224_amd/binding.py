@@ -13,6 +13,7 @@ _lib = None
 
 SYMBOLS = ["nsa_sel_workspace_bytes", "nsa_sel_workspace_bytes_min", "nsa_sel_build_index", "nsa_sel_index_view", "nsa_sel_fwd", "nsa_sel_bwd", "nsa_sel_fwd_static", "nsa_sel_fwd_query_outer", "nsa_sel_fwd_gated", "nsa_sel_bwd_gated", "nsa_sel_select_blocks",
            "nsa_sel_cache_append", "nsa_sel_cache_workspace_bytes", "nsa_sel_cache_attention", "nsa_sel_select_blocks_cached",
+           "nsa_sel_cache_chunk_workspace_bytes", "nsa_sel_cache_attention_chunk", "nsa_sel_cache_read", "nsa_sel_rotary",
            "nsa_sel_profile_enable", "nsa_sel_profile_select", "nsa_sel_profile_collect", "nsa_sel_calibration_copy", "nsa_sel_mfma_probe", "nsa_sel_strerror"]
 
 
@@ -31,6 +32,11 @@ class CacheShape(C.Structure):
     _fields_ = [("n_tokens", C.c_int32), ("nseq", C.c_int32), ("hq", C.c_int32), ("hkv", C.c_int32), ("d", C.c_int32),
                 ("dtype", C.c_int32), ("page", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
                 ("block", C.c_int32), ("topk", C.c_int32), ("window", C.c_int32), ("scale", C.c_float)]
+
+
+class RotaryShape(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("nseq", C.c_int32), ("hq", C.c_int32), ("hkv", C.c_int32), ("d", C.c_int32), ("rot", C.c_int32),
+                ("interleaved", C.c_int32), ("inverse", C.c_int32), ("factor", C.c_double)]
 
 
 def lib():
@@ -57,6 +63,10 @@ def lib():
         L.nsa_sel_cache_workspace_bytes.argtypes = [C.POINTER(CacheShape), C.POINTER(sz)]
         L.nsa_sel_cache_attention.argtypes = [C.POINTER(CacheShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.nsa_sel_select_blocks_cached.argtypes = [C.POINTER(CacheShape), vp, i64, vp, vp, C.c_int32, C.c_int32, vp, vp]
+        L.nsa_sel_cache_chunk_workspace_bytes.argtypes = [C.POINTER(CacheShape), C.POINTER(sz)]
+        L.nsa_sel_cache_attention_chunk.argtypes = [C.POINTER(CacheShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.nsa_sel_cache_read.argtypes = [C.POINTER(CacheShape), vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+        L.nsa_sel_rotary.argtypes = [C.POINTER(RotaryShape), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp]
         L.nsa_sel_profile_enable.argtypes = [C.c_int]
         L.nsa_sel_profile_select.argtypes = [C.c_uint]
         L.nsa_sel_profile_collect.argtypes = [C.c_int, C.POINTER(C.c_char_p), C.POINTER(C.c_float),

@@ -25,6 +25,8 @@ class PagedCache:
         idx = select_blocks(scores, None, topk, kv_len=kv_len)
         o, lse = cache.attention(q, table, kv_len, idx=idx)
 
+    A piece of a prompt is append and attention_chunk; read gives keys and values back as rows.
+
     Forward only: in grad mode tensors that require grad are refused.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
     race, as writes to any tensor do.
 
@@ -100,3 +102,30 @@ class PagedCache:
         out / lse take the results (out may be o_acc); rows of tokens that belong to no sequence are left as they are there, and
         uninitialised otherwise.  ws, of workspace_bytes(), is for callers that may not allocate."""
         return call_native(self._calls.attention, self._device, self._info, q, table, kv_len, cu, idx, block, window, scale, gate, o_acc, out, lse, ws)
+
+    def chunk_workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, window: int = 0) -> int:
+        """Bytes that attention_chunk() of such a call needs as `ws`."""
+        for name, x in dict(tokens=tokens, hq=hq, nseq=nseq, max_pages=max_pages, window=window).items():
+            if not -2 ** 31 <= x < 2 ** 31:
+                raise NsaSelError(f"{name} is out of range")
+        shape = CacheShape(tokens, nseq, hq, self.hkv, _D, int(self.k_pages.dtype is not _BF16), self.page, self.n_pages, max_pages, 64, 0, window, 0.0)
+        need = C.c_size_t()
+        _check(lib().nsa_sel_cache_chunk_workspace_bytes(C.byref(shape), C.byref(need)), "nsa_sel_cache_chunk_workspace_bytes")
+        return need.value
+
+    def attention_chunk(self, q: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *, window: int = 0,
+                        scale: float = 0.0, gate: Optional[torch.Tensor] = None, o_acc: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+        """(O, LSE) as attention() without `idx`, for pieces of prompts: up to 256 / g new tokens of a sequence (g = hq / hkv) share what they read of it.  Right for any
+        numbers of new tokens, faster than attention() from about 16 of a sequence on.  The arguments are those of attention(); ws is of chunk_workspace_bytes()."""
+        return call_native(self._calls.attention_chunk, self._device, self._info, q, table, kv_len, cu, window, scale, gate, o_acc, out, lse, ws)
+
+    def read(self, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *, tokens: Optional[int] = None,
+             k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+        """(K, V) as bfloat16 rows [tokens, hkv, 128]: what the cache holds at the places that an append with the same kv_len and cu would write, the last
+        cu[s + 1] - cu[s] of the kv_len[s] of sequence s.  For whole sequences cu holds the sums of kv_len.  Values in 8 bits come back times their page's scale, exactly.
+
+        tokens, the number of rows (cu[-1], which only the device knows), is needed with cu unless k_out or v_out says it.  k_out / v_out take the results (they may be
+        slices whose tokens lie apart); rows of tokens that belong to no sequence are left as they are there, and uninitialised otherwise.  Rows of negative place, and of
+        places without a page, are zero."""
+        return call_native(self._calls.read, self._device, self._info, table, kv_len, cu, tokens, k_out, v_out)

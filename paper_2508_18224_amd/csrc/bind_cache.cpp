@@ -1,4 +1,4 @@
-// The Python calls over a paged cache (cache.py, select_blocks of binding.py) down to the C ABI: checks of the tensors, outputs and workspace, one call.
+// The Python calls over a paged cache (cache.py, select_blocks of binding.py) and the rotation (rotary.py) down to the C ABI: checks of the tensors, outputs and workspace, one call.
 // A decoding loop makes these calls a few times a layer with a few tokens, and what a call costs on the host is then what it costs: with the checks
 // in Python an append of one token took 10.1 us, its attention 14.7 and its selection 8.4, of which a launch is 3.7; from here 5.6, 10.3 and 5.2.
 // The library knows nothing of this file or of torch.
@@ -411,6 +411,199 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// (info, table, kv_len, cu, tokens, k_out, v_out, stream) -> (K, V)
+PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    count(n, 8);
+    const CacheInfo& c = info(a[0]);
+    const Pages p = pages(c);
+    int64_t T = a[3] == Py_None ? dims(a[1], "table", 2).size(0) : -1;
+    for (int i = 5; i < 7; ++i)
+      if (T < 0 && a[i] != Py_None) T = dims(a[i], i == 5 ? "k_out" : "v_out", 3).size(0);
+    if (a[4] != Py_None) {
+      const int64_t asked = small(a[4], "tokens");
+      if (asked < 0 || (T >= 0 && asked != T)) throw Refused{"tokens must be the number of rows" + (T >= 0 ? ", " + std::to_string(T) : "") + ", got " + std::to_string(asked)};
+      T = asked;
+    }
+    if (T < 0) throw Refused{"tokens (the rows that cu_seqlens counts) is required with cu_seqlens"};
+    const Batch b = batch(a[1], a[2], a[3], T, c.device);
+    const nsa_sel_cache_shape s = shape_of(c, b, T, c.hkv);
+    const int64_t rows[3] = {T, c.hkv, kD};
+    at::Tensor made[2];
+    void* out[2];
+    int64_t stride[2];
+    for (int i = 0; i < 2; ++i) {
+      const char* name = i == 0 ? "k_out" : "v_out";
+      if (a[5 + i] != Py_None) {
+        const at::Tensor& t = tensor(a[5 + i], name);
+        stride[i] = expect_rows(t, name, rows, c.device);
+        out[i] = t.data_ptr();
+      } else {
+        made[i] = empty(rows, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
+        stride[i] = c.hkv * kD;
+        out[i] = made[i].data_ptr();
+      }
+    }
+    on_gpu(c.device);
+    void* const stream = PyLong_AsVoidPtr(a[7]);
+    done(without_gil([&] { return nsa_sel_cache_read(&s, b.cu, b.kv_len, b.table, p.k, p.v, p.ks, p.vs, out[0], stride[0], out[1], stride[1], stream); }),
+         "nsa_sel_cache_read");
+    PyObject* r = PyTuple_New(2);
+    if (!r) throw python_error();
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(r, i, made[i].defined() ? THPVariable_Wrap(std::move(made[i])) : given(a[5 + i]));
+    return r;
+  } catch (const Refused& r) {
+    PyErr_SetString(g_error, r.why.c_str());
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// (info, q, table, kv_len, cu, window, scale, gate, o_acc, out, lse, ws, stream) -> (O, LSE)
+PyObject* attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    count(n, 13);
+    const CacheInfo& c = info(a[0]);
+    const Pages p = pages(c);
+    const at::Tensor& q = dims(a[1], "q", 3);
+    const int64_t T = q.size(0), hq = q.size(1);
+    const int64_t rows[3] = {T, hq, kD}, per_row[2] = {T, hq};
+    const void* q_ptr = expect(q, "q", at::kBFloat16, rows, c.device);
+    const Batch b = batch(a[2], a[3], a[4], T, c.device);
+    nsa_sel_cache_shape s = shape_of(c, b, T, hq);
+    s.window = small(a[5], "window");
+    s.scale = number(a[6]);
+    const float* gate = nullptr;
+    const void* acc = nullptr;
+    if (a[7] != Py_None) {
+      gate = (const float*)expect(tensor(a[7], "gate"), "gate", at::kFloat, per_row, c.device);
+      if (a[8] != Py_None) acc = expect(tensor(a[8], "o_acc"), "o_acc", at::kBFloat16, rows, c.device);
+    } else if (a[8] != Py_None) {
+      throw Refused{"o_acc without gate"};
+    }
+    const auto options = at::TensorOptions().device(c.device);
+    at::Tensor new_o, new_l, new_ws;
+    void *out, *lse, *ws = nullptr;
+    size_t need = 0;
+    done(nsa_sel_cache_chunk_workspace_bytes(&s, &need), "nsa_sel_cache_chunk_workspace_bytes");
+    if (a[11] != Py_None) {
+      const at::Tensor& w = tensor(a[11], "ws");
+      if (w.device() != c.device || !w.is_contiguous()) throw Refused{"ws must be a contiguous tensor on " + c.device.str()};
+      if (w.nbytes() < need) throw Refused{"ws holds " + std::to_string(w.nbytes()) + " bytes, " + std::to_string(need) + " are needed"};
+      ws = w.data_ptr();
+    } else if (need > 0) {
+      new_ws = empty({(int64_t)need}, options.dtype(at::kByte));
+      ws = new_ws.data_ptr();
+    }
+    if (a[9] != Py_None) {
+      out = expect(tensor(a[9], "out"), "out", at::kBFloat16, rows, c.device);
+    } else {
+      new_o = empty(rows, options.dtype(at::kBFloat16));
+      out = new_o.data_ptr();
+    }
+    if (a[10] != Py_None) {
+      lse = expect(tensor(a[10], "lse"), "lse", at::kFloat, per_row, c.device);
+    } else {
+      new_l = empty(per_row, options.dtype(at::kFloat));
+      lse = new_l.data_ptr();
+    }
+    on_gpu(c.device);
+    void* const stream = PyLong_AsVoidPtr(a[12]);
+    done(without_gil([&] {
+           return nsa_sel_cache_attention_chunk(&s, q_ptr, b.cu, b.kv_len, b.table, p.k, p.v, p.ks, p.vs, gate, acc, out, (float*)lse, ws, need, stream);
+         }),
+         "nsa_sel_cache_attention_chunk");
+    PyObject* r = PyTuple_New(2);
+    if (!r) throw python_error();
+    PyTuple_SET_ITEM(r, 0, new_o.defined() ? THPVariable_Wrap(std::move(new_o)) : given(a[9]));
+    PyTuple_SET_ITEM(r, 1, new_l.defined() ? THPVariable_Wrap(std::move(new_l)) : given(a[10]));
+    return r;
+  } catch (const Refused& r) {
+    PyErr_SetString(g_error, r.why.c_str());
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// (q, k, inv_freq, cu, positions, interleaved, factor, inverse, q_out, k_out, stream) -> (rotated q, rotated k or None)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  try {
+    count(n, 11);
+    nsa_sel_rotary_shape s = {};
+    at::Tensor made[2];
+    const void* in[2] = {nullptr, nullptr};
+    void* out[2] = {nullptr, nullptr};
+    int64_t from[2] = {0, 0}, to[2] = {0, 0}, heads[2] = {0, 0};
+    const at::Tensor& q = dims(a[0], "q", 3);
+    const at::Device dev = q.device();
+    const int64_t T = q.size(0);
+    if (T > INT32_MAX) throw Refused{"too many tokens"};
+    for (int i = 0; i < 2; ++i) {
+      const char* name = i == 0 ? "q" : "k";
+      const char* out_name = i == 0 ? "q_out" : "k_out";
+      PyObject* result = a[8 + i];
+      if (a[i] == Py_None) {
+        if (result != Py_None) throw Refused{std::string(out_name) + " without " + name};
+        continue;
+      }
+      const at::Tensor& x = dims(a[i], name, 3);
+      heads[i] = x.size(1);
+      if (heads[i] < 1 || heads[i] > INT32_MAX) throw Refused{std::string(name) + " must have at least one head, got " + text(x.sizes())};
+      const int64_t rows[3] = {T, heads[i], kD};
+      from[i] = expect_rows(x, name, rows, dev);
+      in[i] = x.data_ptr();
+      if (result != Py_None) {
+        const at::Tensor& y = tensor(result, out_name);
+        to[i] = expect_rows(y, out_name, rows, dev);
+        out[i] = y.data_ptr();
+      } else {
+        made[i] = empty(rows, at::TensorOptions().dtype(at::kBFloat16).device(dev));
+        to[i] = heads[i] * kD;
+        out[i] = made[i].data_ptr();
+      }
+    }
+    const at::Tensor& f = dims(a[2], "inv_freq", 1);
+    if (f.size(0) > kD / 2 || f.size(0) % 8) throw Refused{"inv_freq must be float64 [rot / 2], rot a multiple of 16 up to 128, got " + text(f.sizes())};
+    const double* freq = (const double*)expect(f, "inv_freq", at::kDouble, {f.size(0)}, dev);
+    s.n_tokens = (int32_t)T;
+    s.nseq = 1;
+    const void *cu = nullptr, *positions = nullptr;
+    if (a[3] != Py_None) {
+      const at::Tensor& t = dims(a[3], "cu_seqlens", 1);
+      if (t.size(0) < 2 || t.size(0) > INT32_MAX) throw Refused{"cu_seqlens must be int32 [sequences + 1], at least one sequence"};
+      cu = expect(t, "cu_seqlens", at::kInt, {t.size(0)}, dev);
+      s.nseq = (int32_t)(t.size(0) - 1);
+    }
+    if (a[4] != Py_None) positions = expect(dims(a[4], "positions", 1), "positions", at::kInt, {T}, dev);
+    s.hq = (int32_t)heads[0];
+    s.hkv = (int32_t)heads[1];
+    s.d = kD;
+    s.rot = (int32_t)(2 * f.size(0));
+    s.interleaved = truth(a[5]);
+    s.factor = PyFloat_AsDouble(a[6]);
+    if (s.factor == -1.0 && PyErr_Occurred()) throw python_error();
+    if (!(s.factor > 0.0)) throw Refused{"factor must be positive"};
+    s.inverse = truth(a[7]);
+    on_gpu(dev);
+    void* const stream = PyLong_AsVoidPtr(a[10]);
+    done(without_gil([&] {
+           return nsa_sel_rotary(&s, in[0], from[0], in[1], from[1], (const int32_t*)cu, (const int32_t*)positions, freq, out[0], to[0], out[1], to[1], stream);
+         }),
+         "nsa_sel_rotary");
+    PyObject* r = PyTuple_New(2);
+    if (!r) throw python_error();
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(r, i, made[i].defined() ? THPVariable_Wrap(std::move(made[i])) : given(a[i] == Py_None ? Py_None : a[8 + i]));
+    return r;
+  } catch (const Refused& r) {
+    PyErr_SetString(g_error, r.why.c_str());
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_XINCREF(cls);
   Py_XSETREF(g_error, cls);
@@ -420,6 +613,9 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 PyMethodDef kMethods[] = {{"describe", (PyCFunction)(void (*)(void))describe, METH_FASTCALL, nullptr},
                           {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, nullptr},
                           {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, nullptr},
+                          {"read", (PyCFunction)(void (*)(void))read, METH_FASTCALL, nullptr},
+                          {"attention_chunk", (PyCFunction)(void (*)(void))attention_chunk, METH_FASTCALL, nullptr},
+                          {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, nullptr},
                           {"select_blocks", (PyCFunction)(void (*)(void))select_blocks, METH_FASTCALL, nullptr},
                           {"set_error", set_error, METH_O, nullptr},
                           {nullptr, nullptr, 0, nullptr}};

@@ -51,6 +51,22 @@ struct CacheAttend {
 hipError_t launch_cache_attend(const Cache& C, bool e4m3, const CacheAttend& A, hipStream_t st);
 
 #if defined(__HIPCC__)
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Four e4m3 values times 2^e (the exponent of `scale`) as bf16.
+__device__ __forceinline__ uint2 four_bf16(uint32_t x, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+  return {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+}
+__device__ __forceinline__ u32x4 eight_bf16(uint32_t lo, uint32_t hi, float scale) {
+  const uint2 a = four_bf16(lo, scale), b = four_bf16(hi, scale);
+  return u32x4{a.x, a.y, b.x, b.y};
+}
+
 // The s with base(s) <= u < base(s + 1) of a non-decreasing base: [0, n) is cut into 64 by the wavefront's lanes in every round.  -1 where
 // u is outside.  All lanes of the wavefront take part and get the same result.
 template <class Base>

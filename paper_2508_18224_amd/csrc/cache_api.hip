@@ -1,64 +1,8 @@
 // C ABI of the calls over a paged cache (see include/nsa_sel.h): argument validation, workspace size, launch parameters.
-#include "cache.h"
+#include "cache_checks.h"
 
 namespace nsa {
 namespace {
-
-bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-// 16 bytes for tensors; null only where `or_null`
-bool tensor(const void* p, bool or_null = false) { return p ? aligned(p, 16) : or_null; }
-bool ints(const void* p, bool or_null = false) { return p ? aligned(p, 4) : or_null; }
-
-int check_sizes(const nsa_sel_cache_shape* s, bool attention) {
-  if (!s) return NSA_SEL_EINVAL;
-  if (s->n_tokens < 0 || s->nseq < 0 || (s->nseq == 0 && s->n_tokens > 0) || s->hq < 1 || s->hkv < 1 || s->n_pages < 0 || s->max_pages < 0)
-    return NSA_SEL_EINVAL;
-  if (s->hq % s->hkv != 0 || s->hq / s->hkv > 8) return NSA_SEL_EINVAL;
-  if (s->dtype != NSA_SEL_CACHE_BF16 && s->dtype != NSA_SEL_CACHE_E4M3) return NSA_SEL_EINVAL;
-  if (attention && s->window < 0) return NSA_SEL_EINVAL;
-  if (s->d != kD || s->page < 16 || s->page > 256 || (s->page & (s->page - 1)) != 0) return NSA_SEL_EUNSUPPORTED;
-  if ((int64_t)s->max_pages * s->page > (1 << 30)) return NSA_SEL_EUNSUPPORTED;  // places are 32-bit numbers
-  if (s->nseq > (1 << 24) || (int64_t)s->n_tokens * s->hq >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;
-  if (attention) {
-    if (s->topk < 0 || s->topk > kMaxTopk) return NSA_SEL_EUNSUPPORTED;
-    if (s->topk > 0 && s->block != kBlock && s->block != 2 * kBlock) return NSA_SEL_EUNSUPPORTED;
-  }
-  return NSA_SEL_OK;
-}
-
-Cache make_cache(const nsa_sel_cache_shape* s, const void* k, const void* v, const float* ks, const float* vs, const int32_t* table,
-                 const int32_t* kv_len, const int32_t* cu) {
-  Cache C;
-  C.k = (char*)const_cast<void*>(k);
-  C.v = (char*)const_cast<void*>(v);
-  C.ks = const_cast<float*>(ks);
-  C.vs = const_cast<float*>(vs);
-  C.table = table;
-  C.kv_len = kv_len;
-  C.cu = cu;
-  C.T = s->n_tokens;
-  C.nseq = s->nseq;
-  C.hq = s->hq;
-  C.hkv = s->hkv;
-  C.g = s->hq / s->hkv;
-  C.n_pages = s->n_pages;
-  C.max_pages = s->max_pages;
-  C.page_log2 = __builtin_ctz((unsigned)s->page);
-  return C;
-}
-
-int check_cache_pointers(const nsa_sel_cache_shape* s, const void* k, const void* v, const float* ks, const float* vs,
-                         const int32_t* table, const int32_t* kv_len, const int32_t* cu) {
-  if (!ints(kv_len) || !ints(cu, true) || !ints(table, s->max_pages == 0)) return NSA_SEL_EINVAL;
-  if (!cu && s->nseq != s->n_tokens) return NSA_SEL_EINVAL;
-  const bool none = s->n_pages == 0;
-  if (!tensor(k, none) || !tensor(v, none)) return NSA_SEL_EINVAL;
-  if (s->dtype == NSA_SEL_CACHE_E4M3 && (!ints(ks, none) || !ints(vs, none))) return NSA_SEL_EINVAL;
-  return NSA_SEL_OK;
-}
-
-// No place is as far back as 2^30 of another: a window that long is none, and the kernels' sums with one stay in 32 bits.
-int32_t window_of(const nsa_sel_cache_shape* s) { return s->window < (1 << 30) ? s->window : 0; }
 
 // How the attention is cut (see launch_cache_attend).
 struct Cut {

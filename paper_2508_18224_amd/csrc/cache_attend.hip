@@ -30,12 +30,6 @@ static_assert(kPiece * kVRow <= kOwnLds, "the tile of a wavefront must fit");
 static_assert(64 * kWaves == kAttendThreads, "the host reckons with this many");
 static_assert(kTiles == 2, "a piece is one contraction step of the PV product");
 
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // A row of the call: `nt` consecutive new tokens t0.. of sequence s, the first of them at `place`, and KV head j.
 struct Row {
   int s, t0, nt, place, j;
@@ -92,16 +86,6 @@ __device__ __forceinline__ void load_values(const Cache& C, const Piece& P, int 
 #pragma unroll
     for (int s = 0; s < kN; ++s) r.x[i * kN + s] = __builtin_amdgcn_raw_buffer_load_b128(b, 1024 * s + lane * 16, 0, kPolicy);
   }
-}
-
-// Four e4m3 values times 2^e (the exponent of `scale`) as bf16.
-__device__ __forceinline__ uint2 four_bf16(uint32_t x, float scale) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
-  return {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-}
-__device__ __forceinline__ u32x4 eight_bf16(uint32_t lo, uint32_t hi, float scale) {
-  const uint2 a = four_bf16(lo, scale), b = four_bf16(hi, scale);
-  return u32x4{a.x, a.y, b.x, b.y};
 }
 
 // Row b of a call that gives every workgroup a row; s < 0 where there is none.

@@ -215,7 +215,7 @@ inline int64_t bwd_units_min(int b_cap, int T, int topk, int unit) {
 enum KernelId {
   KID_INDEX_PREP = 0, KID_INDEX_HIST, KID_INDEX_DENSE, KID_INDEX_SCAN, KID_INDEX_SCATTER, KID_FWD_MAIN, KID_FWD_MERGE,
   KID_FWD_DENSE, KID_FWD_SHORT, KID_FWD_QUERY_OUTER, KID_BWD_DELTA, KID_BWD_MAIN, KID_BWD_DQ_REDUCE, KID_BWD_DKV_REDUCE, KID_SELECT_BLOCKS,
-  KID_CACHE_APPEND, KID_CACHE_ATTEND, KID_CACHE_JOIN,
+  KID_CACHE_APPEND, KID_CACHE_ATTEND, KID_CACHE_JOIN, KID_CACHE_CHUNK, KID_CACHE_CHUNK_JOIN, KID_CACHE_READ, KID_ROTARY,
   KID_COUNT
 };
 // Records a HIP event on `st` at construction and destruction when profiling is on; does nothing otherwise.

@@ -16,7 +16,7 @@ unsigned g_mask = ~0u;  // kernel kinds that are recorded (bit = index in kNames
 const char* const kNames[KID_COUNT] = {"index_prep", "index_hist", "index_dense", "index_scan", "index_scatter", "fwd_main",
                                        "fwd_merge", "fwd_dense", "fwd_short", "fwd_query_outer", "bwd_delta", "bwd_main",
                                        "bwd_dq_reduce", "bwd_dkv_reduce", "select_blocks", "cache_append", "cache_attend",
-                                       "cache_join"};
+                                       "cache_join", "cache_chunk", "cache_chunk_join", "cache_read", "rotary"};
 }  // namespace
 
 ProfScope::ProfScope(int kid, hipStream_t stream) : slot(-1), st(stream) {
