@@ -23,8 +23,7 @@ __device__ __forceinline__ void piece_addresses(uint32_t k_lds, uint32_t v_lds, 
 }
 
 // S^T = K Q^T of the piece: lane = row, register v of half mb = key 32 mb + 8 (v >> 2) + 4 qh + (v & 3).
-template <class KAddr>
-__device__ __forceinline__ void piece_scores(const KAddr& kaddr, const bf16x8 (&qf)[8], f32x16 (&sacc)[2]) {
+__device__ __forceinline__ void piece_scores(const uint32_t (&kaddr)[8], const bf16x8 (&qf)[8], f32x16 (&sacc)[2]) {
 #pragma unroll
   for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
@@ -91,6 +90,7 @@ __device__ __forceinline__ bf16x8 piece_probabilities(const f32x16 (&sacc)[2], i
   return pf;
 }
 
+// VAddr: the addresses as piece_addresses gives them, or what makes them when they are asked for.
 template <class VAddr>
 __device__ __forceinline__ bf16x8 value_frag(const VAddr& vaddr, int sp, int db) {
   const bf16x4 a0 = lds_read_tr_at(vaddr[0][db] + 16 * sp * kPieceRow), a1 = lds_read_tr_at(vaddr[1][db] + 16 * sp * kPieceRow);
@@ -103,9 +103,8 @@ __device__ __forceinline__ bf16x8 value_frag(const VAddr& vaddr, int sp, int db)
 // sums before the PV product and whatever `beside(step)` issues: the loads of pieces to come, which would hold the wavefront up if they were issued at once.  Without
 // the rescale it measured 1040 clocks, of which the products need 1024; with it the kernels take 0.5 % (k_fwd_dense_merge, nine pieces) to 6 %
 // (k_fwd_short, 6000 tokens) longer.
-// KAddr, VAddr: the addresses as piece_addresses gives them, or what makes them when they are asked for.  kRescale: the sums are multiplied by alpha here; else they have been.
-template <bool kRescale = true, class KAddr, class VAddr, class Beside>
-__device__ __forceinline__ float piece_values_and_next_scores(const KAddr& kaddr, const VAddr& vaddr,
+template <class Beside>
+__device__ __forceinline__ float piece_values_and_next_scores(const uint32_t (&kaddr)[8], const uint32_t (&vaddr)[2][4],
                                                               const bf16x8 (&qf)[8], float c2, float mc, float alpha, const f32x16 (&cur)[2],
                                                               f32x16 (&next)[2], float& l_run, f32x16 (&oacc)[4], Beside beside) {
   constexpr int kAhead = 4;
@@ -128,7 +127,7 @@ __device__ __forceinline__ float piece_values_and_next_scores(const KAddr& kaddr
     else oacc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % kAhead], pf[(i - 16) >> 2], oacc[i & 3], 0, 0, 0);
     if (i + kAhead < 32) frag[i % kAhead] = read(i + kAhead);
     beside(i);
-    if (kRescale && i < 16) {
+    if (i < 16) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) oacc[i >> 2][4 * (i & 3) + v] *= alpha;
     }
@@ -154,8 +153,7 @@ __device__ __forceinline__ float piece_values_and_next_scores(const KAddr& kaddr
 }
 
 // The same for the last piece, after which no scores are wanted.
-template <class VAddr>
-__device__ __forceinline__ void piece_values(const VAddr& vaddr, float c2, float mc, float alpha, const f32x16 (&cur)[2],
+__device__ __forceinline__ void piece_values(const uint32_t (&vaddr)[2][4], float c2, float mc, float alpha, const f32x16 (&cur)[2],
                                              float& l_run, f32x16 (&oacc)[4]) {
   float l = 0.f;
 #pragma unroll

@@ -86,14 +86,13 @@ def test_attention_of_pieces_refuses():
     assert _chunk(empty, q=None, cu=None, n=None, t=None, kp=None, vp=None, o=None, lse=None, ws=None, ws_bytes=0) == OK
 
 
-def test_sizes_that_no_launch_holds():
-    """The launch that joins parts: a workgroup of 256 for 32 rows."""
-    s = _shape(nsa, n_tokens=(1 << 26) - 1, nseq=1, hq=8, hkv=1, topk=0)
-    assert _need(s)[0] == UNSUPPORTED and _chunk(s) == UNSUPPORTED
-    s = _shape(nsa, n_tokens=1 << 20, nseq=1 << 20, hq=1, hkv=1, topk=0)
-    assert _need(s)[0] == OK
-    s = _shape(nsa, n_tokens=1 << 24, nseq=1 << 24, hq=1, hkv=1, topk=0)
-    assert _need(s)[0] == UNSUPPORTED
+def test_workspace_of_the_largest_calls():
+    """The launches do not grow with the call: the workspace is the same for every size."""
+    sizes = {_need(_shape(nsa, topk=0, **kw)) for kw in (dict(n_tokens=1, nseq=1, hq=8, hkv=8), dict(n_tokens=(1 << 28) - 1, nseq=1, hq=8, hkv=1),
+                                                        dict(n_tokens=1 << 24, nseq=1 << 24, hq=64, hkv=8), dict(n_tokens=(1 << 31) - 1, nseq=1 << 24, hq=1, hkv=1))}
+    assert len(sizes) == 1 and sizes.pop()[0] == OK
+    assert _need(_shape(nsa, n_tokens=1 << 28, nseq=1, hq=8, hkv=1, topk=0))[0] == UNSUPPORTED
+    assert _need(_shape(nsa, n_tokens=1 << 25, nseq=(1 << 24) + 1, hq=1, hkv=1, topk=0))[0] == UNSUPPORTED
 
 
 # ---- the Python calls ----------------------------------------------------------------------------------------------------------
