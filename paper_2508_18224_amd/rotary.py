@@ -25,21 +25,24 @@ def _call(q, k, inv_freq, cu, positions, interleaved, factor, inverse, q_out=Non
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, inv_freq, cu, positions, interleaved, factor, inverse):
-        ctx.save_for_backward(inv_freq, cu, positions)
-        ctx.how = interleaved, factor, not inverse
+    def forward(ctx, q, k, *how):
+        ctx.save_for_backward(*how[:3])
+        ctx.how = how[3:]
         ctx.set_materialize_grads(False)
-        return _call(q, k, inv_freq, cu, positions, interleaved, factor, inverse)
+        return _call(q, k, *how)
 
     @staticmethod
     def backward(ctx, dq, dk):
         """The gradients turned back; differentiable itself, as the rotation is linear."""
-        inv_freq, cu, positions = ctx.saved_tensors
-        given = [g if need else None for g, need in zip((dq, dk), ctx.needs_input_grad)]
-        turn = [_rows(g) for g in given if g is not None]
-        if turn:
-            turn = list(_Rotary.apply(turn[0], turn[1] if len(turn) > 1 else None, inv_freq, cu, positions, *ctx.how))
-        return (*(None if g is None else turn.pop(0) for g in given), None, None, None, None, None, None)
+        need_q, need_k = ctx.needs_input_grad[:2]
+        dq, dk = _rows(dq) if need_q and dq is not None else None, _rows(dk) if need_k and dk is not None else None
+        turn = _Rotary.apply if torch.is_grad_enabled() else _call  # (a node of its own only where somebody may want it)
+        interleaved, factor, inverse = ctx.how
+        if dq is not None:
+            dq, dk = turn(dq, dk, *ctx.saved_tensors, interleaved, factor, not inverse)
+        elif dk is not None:
+            dk = turn(dk, None, *ctx.saved_tensors, interleaved, factor, not inverse)[0]
+        return dq, dk, None, None, None, None, None, None
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
