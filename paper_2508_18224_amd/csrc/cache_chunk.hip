@@ -6,8 +6,8 @@
 // LDS as long.
 //
 // What bounds it is power before the pipes: with random numbers the products of a piece and their operand reads alone take 1.34 us, at 1.7 GHz, which is what a large library product
-// reaches too (1.6 PFLOP/s); moving K and V adds 0.14 and the softmax 0.3, as if each were paid for by itself.  2048 new tokens of 32 heads behind 32768 keys (8 KV heads): 1.02 ms,
-// 1.11 PFLOP/s.
+// reaches too (1.6 PFLOP/s); moving K and V adds 0.14 and the softmax 0.3, as if each were paid for by itself.  2048 new tokens of 32 heads behind 32768 keys (8 KV heads): 1.0 ms,
+// 1.13 PFLOP/s.  (64 rows a wavefront, half the operand reads: 1.34 us as well.)
 //
 // A page of 16 tokens or more is a run of memory, so the eight rows that a wavefront moves of a piece's K and V are always one page's: which one is looked up for 64 pieces
 // at a time, a piece a lane.
@@ -26,8 +26,10 @@ constexpr int kChunkWaves = 8, kChunkRows = 32 * kChunkWaves, kChunkThreads = 64
 constexpr int kStages = 4;  // tiles of K, and of V: one more than a piece that is asked for two before it is used needs, so that nobody waits for the tile to be free
 constexpr int kChunkV = kStages * kPieceBytes, kChunkLds = 2 * kStages * kPieceBytes + 64;
 constexpr int kSlots = 256;  // workgroups that share all units' pieces evenly
-constexpr int kUnitCost = 5;  // what a unit costs beside its pieces, in pieces: its Q, its pages, the first and last piece, its result
-constexpr int kLeastSpan = 2, kLeastShare = 7;  // (4, 9, 12: 27, 26 and 28.5 us for 16 tokens behind 4080 keys, 7: 24.7)
+// What a unit costs beside its pieces, in pieces: its Q, its pages, the first and the last piece, its result, 10 to 12 us for 1.9 of a piece.  (A whole prompt of 8192 tokens: 1300 us
+// with none of it counted, 1023 with 5, 1004 with 6, 1013 with 8.)
+constexpr int kUnitCost = 6;
+constexpr int kLeastSpan = 2, kLeastShare = 6;  // (16 tokens behind 4080 keys: 23.6 us with 5 or 6 to a workgroup, 24.7 with 7, 28.5 with 12)
 constexpr int kChunkJoinThreads = 512;
 static_assert(kChunkRows * kPieceRow <= kChunkLds, "the result must fit where the tiles were");
 
