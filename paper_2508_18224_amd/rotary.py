@@ -1,5 +1,5 @@
 """Rotary positions for queries and keys of the training path (nsa_sel_rotary of include/nsa_sel.h, which states the rules).  Arguments are checked and handed to the
-library in csrc/bind_cache.cpp; no arithmetic on tensors happens here."""
+library in csrc/bind_cache.cpp, which has the gradient too; no arithmetic on tensors happens here."""
 from __future__ import annotations
 
 import math
@@ -8,41 +8,6 @@ from typing import Optional
 import torch
 
 from .binding import NsaSelError, call_native, native
-
-
-def _rows(x: torch.Tensor) -> torch.Tensor:
-    """x, or a copy of it where its rows do not lie as the library takes them (gradients come as autograd made them: expanded, transposed)."""
-    T, h, d = x.shape
-    fits = x.stride(2) == 1 and (h == 1 or x.stride(1) == d) and (T == 1 or (x.stride(0) >= h * d and x.stride(0) % 8 == 0)) and x.data_ptr() % 16 == 0
-    return x if fits else x.contiguous()
-
-
-def _call(q, k, inv_freq, cu, positions, interleaved, factor, inverse, q_out=None, k_out=None):
-    if not isinstance(q, torch.Tensor):
-        raise NsaSelError("q must be a torch.Tensor")
-    return call_native(native().rotary, q.device, q, k, inv_freq, cu, positions, interleaved, factor, inverse, q_out, k_out)
-
-
-class _Rotary(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, q, k, *how):
-        ctx.save_for_backward(*how[:3])
-        ctx.how = how[3:]
-        ctx.set_materialize_grads(False)
-        return _call(q, k, *how)
-
-    @staticmethod
-    def backward(ctx, dq, dk):
-        """The gradients turned back; differentiable itself, as the rotation is linear."""
-        need_q, need_k = ctx.needs_input_grad[:2]
-        dq, dk = _rows(dq) if need_q and dq is not None else None, _rows(dk) if need_k and dk is not None else None
-        turn = _Rotary.apply if torch.is_grad_enabled() else _call  # (a node of its own only where somebody may want it)
-        interleaved, factor, inverse = ctx.how
-        if dq is not None:
-            dq, dk = turn(dq, dk, *ctx.saved_tensors, interleaved, factor, not inverse)
-        elif dk is not None:
-            dk = turn(dk, None, *ctx.saved_tensors, interleaved, factor, not inverse)[0]
-        return dq, dk, None, None, None, None, None, None
 
 
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
@@ -56,11 +21,10 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Tensor, c
     sequence), or what positions (int32 [tokens]) says, beside which cu is not looked at.  Tokens of no sequence are copied as they are.
 
     q_out / k_out take the results where no gradient is wanted (they may be q / k themselves)."""
-    if q_out is not None or k_out is not None or not torch.is_grad_enabled():
-        return _call(q, k, inv_freq, cu, positions, interleaved, factor, False, q_out, k_out)
-    if not any(isinstance(x, torch.Tensor) and x.requires_grad for x in (q, k)):
-        return _call(q, k, inv_freq, cu, positions, interleaved, factor, False)
-    return _Rotary.apply(q, k, inv_freq, cu, positions, interleaved, factor, False)
+    if not isinstance(q, torch.Tensor):
+        raise NsaSelError("q must be a torch.Tensor")
+    node = q_out is None and k_out is None and torch.is_grad_enabled() and (q.requires_grad or (isinstance(k, torch.Tensor) and k.requires_grad))
+    return call_native(native().rotary, q.device, q, k, inv_freq, cu, positions, interleaved, factor, False, q_out, k_out, node)
 
 
 def rotary_frequencies(rot: int = 128, base: float = 10000.0, *, scaling: Optional[str] = None, stretch: float = 1.0, trained: int = 8192,

@@ -126,6 +126,40 @@ def test_a_captured_backward_pass():
             assert torch.equal(a, c)
 
 
+def test_gradients_as_a_program_may_ask_for_them():
+    """Twice of one pass; on a stream of its own; for one input; through a hook; not after the graph is gone or after the places were changed."""
+    q, k, g = (torch.randn(90, h, 128, device="cuda").to(torch.bfloat16) for h in (HQ, HKV, HQ))
+    places = torch.arange(90, dtype=torch.int32, device="cuda") * 3
+    f, _ = nsa.rotary_frequencies(96, device="cuda")
+    want = nsa.rotary(g, None, -f, positions=places)[0]
+    a = q.clone().requires_grad_()
+    x, y = nsa.rotary(a, k, f, positions=places)
+    assert x.requires_grad and x.grad_fn is not None
+    for _ in range(2):
+        assert torch.equal(torch.autograd.grad(x, a, g, retain_graph=True)[0], want)
+    seen = []
+    x.register_hook(lambda grad: seen.append(grad) or 2 * grad)
+    assert torch.equal(torch.autograd.grad(x, a, g)[0], nsa.rotary(2 * g, None, -f, positions=places)[0]) and torch.equal(seen[0], g)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(x, a, g)                                  # the graph is gone
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        b = q.detach().clone().requires_grad_()
+        x, _ = nsa.rotary(b, k, f, positions=places)
+        (d,) = torch.autograd.grad(x, b, g)
+    assert not s.query()
+    s.synchronize()
+    assert torch.equal(d, want)
+    with torch.no_grad():
+        assert not nsa.rotary(a, k, f, positions=places)[0].requires_grad
+    x, _ = nsa.rotary(a, k, f, positions=places)
+    places.add_(1)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(x, a, g)                                  # the places of the pass are no longer there
+
+
 def test_two_graphs_and_an_eager_call_at_once():
     """Workspaces of calls that run beside each other are apart."""
     batches = [Batch(160 + i, [3000 - 700 * i, 70, 1900], [50, 70, 33 + i], hq=HQ, hkv=HKV, page=64, e4m3=i == 1) for i in range(2)]
