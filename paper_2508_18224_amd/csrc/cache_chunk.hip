@@ -596,8 +596,9 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {  // a value that all lan
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 struct State {
-  int s, i, j, pad;        // the unit
-  int64_t q, left, share;  // where the workgroup begins in it, what is left to be done, what a workgroup does; in pieces
+  int s, i, j, t0, nt, place;  // the unit
+  int64_t q, left;             // where the workgroup begins in it, what is left to be done, in pieces
+  int share;                   // what a workgroup does, where that is less than 2^31
 };
 // Where a unit of this cost is cut if an equal share ends at x: not so near its ends that a part of it would cost more than it is worth.
 __device__ __forceinline__ int64_t cut_at(int64_t x, int64_t cost) { return x < kUnitCost + kLeastSpan ? 0 : x > cost - kLeastSpan ? cost : x; }
@@ -626,22 +627,29 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
       const int64_t i = u - first_unit(C, A, s);
       if (i < 0) continue;
       const Unit W = unit_of(C, A, s, (int)i, 0);
-      if (W.s >= 0 && !visit(s, (int)i, kUnitCost + pieces_of(C, A, W).y)) return;
+      if (W.s >= 0 && !visit(W, (int)i, kUnitCost + pieces_of(C, A, W).y)) return;
     }
   };
   int64_t own = 0;
-  each_unit([&](int, int, int n) {
-    own += n;
+  Unit head;  // the first of them
+  int head_i = 0, head_cost = 0;
+  each_unit([&](const Unit& W, int i, int cost) {
+    if (own == 0) {
+      head = W;
+      head_i = i;
+      head_cost = cost;
+    }
+    own += cost;
     return true;
   });
   int64_t upto = own;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
+  for (int d = 1; d < 64 && d < A.units; d <<= 1) {
     const int64_t x = __shfl_up(upto, d);
     if (lane >= d) upto += x;
   }
   int64_t* sums = reinterpret_cast<int64_t*>(smem);
-  if (lane == 63) sums[wave] = upto;
+  if (lane == 63) sums[wave] = A.units < 64 ? 0 : upto;
+  if (A.units < 64 && threadIdx.x == A.units - 1) sums[0] = upto;
   __syncthreads();
   int64_t before = upto - own, of_head = 0;
 #pragma unroll
@@ -653,34 +661,31 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
   const int64_t total = of_head * C.hkv, share = max((total + kSlots - 1) / kSlots, (int64_t)kLeastShare), start = wg * share;
   if (threadIdx.x == 0) A.joints[wg].parts = 0;
   if (start >= total) return;  // the whole workgroup
-  int j = (int)(start / of_head);
+  const int j = total < (int64_t)1 << 32 ? (int)((uint32_t)start / (uint32_t)of_head) : (int)(start / of_head);
   const int64_t at = start - j * of_head;
-  if (before <= at && at < before + own) {
-    int64_t sum = before;
-    each_unit([&](int s, int i, int n) {
-      if (at < sum + n) {
-        sums[kChunkWaves] = (int64_t)s << 32 | (uint32_t)i;
-        sums[kChunkWaves + 1] = at - sum;
-        return false;
-      }
-      sum += n;
-      return true;
-    });
-  }
   // Where the workgroup stands lies in LDS behind the tiles, and not in registers that the units want
   State* state = reinterpret_cast<State*>(smem + 2 * kStages * kPieceBytes);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const int64_t si = sums[kChunkWaves];
-    *state = State{(int)(si >> 32), (int)si, j, 0, sums[kChunkWaves + 1], min(share, total - start), share};
+  if (before <= at && at < before + own) {
+    int64_t sum = before;
+    auto here = [&](const Unit& W, int i, int cost) {
+      if (at < sum + cost) {
+        *state = State{W.s, i, j, W.t0, W.nt, W.place, at - sum, min(share, total - start), (int)min(share, (int64_t)INT32_MAX)};
+        return false;
+      }
+      sum += cost;
+      return true;
+    };
+    if (here(head, head_i, head_cost)) {
+      sum = before;
+      each_unit(here);
+    }
   }
   __syncthreads();
   for (;;) {
     {
       const Cache& C = arguments().C;
       const ChunkArgs& A = arguments().A;
-      const int s = __builtin_amdgcn_readfirstlane(state->s), i = __builtin_amdgcn_readfirstlane(state->i);
-      const Unit W = unit_of(C, A, s, i, __builtin_amdgcn_readfirstlane(state->j));
+      const Unit W = {state->s, state->t0, state->nt, state->place, state->j};
       const int64_t q = uniform(state->q), left = uniform(state->left);
       const int n = pieces_of(C, A, W).y;
       const int64_t cost = kUnitCost + n, begin = cut_at(q, cost), end = q + left >= cost ? cost : cut_at(q + left, cost);
@@ -692,7 +697,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
       P.slot = 2 * wg + (begin == 0 ? 1 : 0);
       if (begin == 0 && 0 < end && end < cost && threadIdx.x == 0) {
         // the others' parts: one for each cut of the unit
-        A.joints[wg] = Joint{W.t0, W.nt, W.j, 2 + (int)((cost - kLeastSpan - end) / state->share), P.slot, 2 * (wg + 1), {0, 0}};
+        A.joints[wg] = Joint{W.t0, W.nt, W.j, 2 + (int)((uint32_t)(cost - kLeastSpan - end) / (uint32_t)state->share), P.slot, 2 * (wg + 1), {0, 0}};
       }
       __syncthreads();  // all have read the state
       if (threadIdx.x == 0) {
@@ -718,11 +723,15 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
       i = 0;
       if (s < 0 || j >= C.hkv) return;  // (starts that are not in order)
     }
+    const Unit W = unit_of(C, A, s, i, j);
     __syncthreads();  // all have read the state
     if (threadIdx.x == 0) {
       state->s = s;
       state->i = i;
       state->j = j;
+      state->t0 = W.t0;
+      state->nt = W.nt;
+      state->place = W.place;
     }
     __syncthreads();
   }

@@ -315,6 +315,20 @@ def test_largest_values():
         check_chunks(o[rows], lse[rows], tuple(x[rows] for x in ref), keys=700, most=most)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_results_in_place_of_the_sum_so_far(e4m3):
+    """out may be o_acc: units that one workgroup has, and such as are joined from parts."""
+    b = Batch(174, [5000, 300, 64], [40, 130, 64], hq=8, hkv=2, page=32, e4m3=e4m3)
+    cache = b.upload(nsa)
+    gate = torch.rand(b.T, 8, device="cuda")
+    acc = torch.randn(b.T, 8, 128, device="cuda").to(torch.bfloat16)
+    for window in (0, 90):
+        want, lse = cache.attention_chunk(b.dq, b.dtable, b.dlen, b.dcu, window=window, gate=gate, o_acc=acc)
+        both = acc.clone()
+        got = cache.attention_chunk(b.dq, b.dtable, b.dlen, b.dcu, window=window, gate=gate, o_acc=both, out=both)
+        assert got[0] is both and torch.equal(both, want) and torch.equal(got[1], lse)
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_drawn_by_lot(seed):
     """Heads, pages, lengths, windows, gates, both formats, rotations of every kind."""
