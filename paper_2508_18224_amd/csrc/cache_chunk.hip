@@ -5,9 +5,9 @@
 // SIMD, each with its Q and its output in registers, share a piece's K and V in LDS.  A piece is 32 KB and 8.4 MFLOP, 2048 clocks of the matrix pipes; reading its operands takes the
 // LDS as long.
 //
-// What bounds it is power before the pipes: with random numbers the products of a piece and their operand reads alone take 1.34 us, at 1.7 GHz, which is what a large library product
-// reaches too (1.6 PFLOP/s); moving K and V adds 0.14 and the softmax 0.3, as if each were paid for by itself.  2048 new tokens of 32 heads behind 32768 keys (8 KV heads): 1.0 ms,
-// 1.13 PFLOP/s.  (64 rows a wavefront, half the operand reads: 1.34 us as well.)
+// What bounds it is power and the vector phase before the pipes: with random numbers the products of a piece and their operand reads alone take 1.23 us, at 1.7 GHz; with moving K and V
+// and the softmax it is 1.68 at 2.1 GHz, 3570 clocks, of which a wavefront's vector phase is 1760 and its matrix phase 1500, beside another's vector phase.  A large library product reaches 1.6
+// PFLOP/s; 2048 new tokens of 32 heads behind 32768 keys (8 KV heads) take 0.94 to 0.99 ms, 1.15 to 1.2 PFLOP/s.
 //
 // A page of 16 tokens or more is a run of memory, so the eight rows that a wavefront moves of a piece's K and V are always one page's: which one is looked up for 64 pieces
 // at a time, a piece a lane.
@@ -93,20 +93,14 @@ __device__ __forceinline__ int2 pieces_of(const Cache& C, const ChunkArgs& A, co
   return {first, max((hi + 63) / 64 - first, 0)};
 }
 
-// This lane's operand reads as piece_addresses has them.  Tiles lie at multiples of 256 bytes, so that the reads of a piece differ in bits that are flipped: made anew from
-// one address, they take no registers.
-struct KeyAddresses {
-  uint32_t at;
-  __device__ __forceinline__ uint32_t operator[](int s) const { return at ^ (s << 5); }
-};
-struct ValueAddresses {
-  uint32_t at;
-  struct Half {
-    uint32_t at;
-    __device__ __forceinline__ uint32_t operator[](int d) const { return at ^ (d << 6); }
-  };
-  __device__ __forceinline__ Half operator[](int h) const { return {h ? (at ^ 32) + 8 * kPieceRow : at}; }
-};
+// Operand reads of a piece (see row_turn: keys' rows turned by four bits, so that reads of a piece differ in bits that are flipped, and take no registers when made anew from one address).
+// Keys: of 16 rows, lane l the row l % 16, channels 8 (l / 16) .. of step s of the contraction.  Values: transposed, 16 channels, keys 4 (l / 16) .. of two groups of 16.
+__device__ __forceinline__ bf16x8 key_operand(uint32_t at, int s, int group) { return lds_read_frag((at ^ (s << 6)) + 16 * group * kPieceRow); }
+__device__ __forceinline__ bf16x8 value_operand(uint32_t at, int sp, int db) {
+  const uint32_t a = (at ^ (db << 5)) + 32 * sp * kPieceRow;
+  const bf16x4 a0 = lds_read_tr_at(a), a1 = lds_read_tr_at(a + 16 * kPieceRow);
+  return __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
 // threadIdx.x & 63, made anew wherever it is asked for: what derives from it need not be kept.
 __device__ __forceinline__ int own_lane() {
@@ -114,16 +108,16 @@ __device__ __forceinline__ int own_lane() {
   asm volatile("" : "+v"(tid));
   return tid & 63;
 }
-// This lane's row of a wavefront's 32: token of the unit and row of Q and O.  Lanes past the last row go along with it.
+// This lane's row x of a wavefront's 32, a lane having two, l % 16 and 16 on: token of the unit and row of Q and O.  Lanes past the last row go along with it.
 struct LaneRow {
   int r, token;
   int64_t row;
   bool here;
 };
-__device__ __forceinline__ LaneRow lane_row(const Cache& C, const ChunkArgs& A, const Unit& W, int wave) {
+__device__ __forceinline__ LaneRow lane_row(const Cache& C, const ChunkArgs& A, const Unit& W, int wave, int x) {
   LaneRow L;
   const int rows = W.nt * C.g;
-  L.r = 32 * wave + (own_lane() & 31);
+  L.r = 32 * wave + 16 * x + (own_lane() & 15);
   L.here = L.r < rows;
   const int rc = min(L.r, rows - 1);
   L.token = div_g(rc, C.g, A.g_magic);
@@ -145,12 +139,29 @@ __device__ __forceinline__ float new_reference(float m, float& ref, float& alpha
 // A reference need not be the maximum: probabilities up to 2^kSlack are as good as those up to 1, and the sums are rescaled far more seldom.
 constexpr float kSlack = 6.f;
 
-// Maximum of this lane's value and that of the lane 32 on or back, which has the same row.
-__device__ __forceinline__ float both_halves_max(float m) {
-  const uint32_t x = __builtin_bit_cast(uint32_t, m);
-  const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  const uint32_t low = y[0], high = y[1];  // (by way of integers: a bit cast of an element takes the first one)
-  return fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
+// The two rows of a lane are those of three others too (l % 16).  What there is one of for a row, the lower half of the lanes has for the first rows, the upper half for the second ones.
+struct Two {
+  float x, y;
+};
+__device__ __forceinline__ Two swap_32(float a, float b) {  // lower half: (a, a of the lane 32 on); upper half: (b of the lane 32 back, b)
+  const auto z = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+  const uint32_t low = z[0], high = z[1];  // (by way of integers: a bit cast of an element takes the first one)
+  return {__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+__device__ __forceinline__ Two both_rows(float x) { return swap_32(x, x); }  // the first rows' and the second rows', in all lanes
+__device__ __forceinline__ Two swap_16(float a) {
+  const uint32_t x = __builtin_bit_cast(uint32_t, a);
+  const auto z = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  const uint32_t low = z[0], high = z[1];
+  return {__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+__device__ __forceinline__ float row_max(float a, float b) {
+  const Two h = swap_32(a, b), q = swap_16(fmaxf(h.x, h.y));
+  return fmaxf(q.x, q.y);
+}
+__device__ __forceinline__ float row_sum(float a, float b) {
+  const Two h = swap_32(a, b), q = swap_16(h.x + h.y);
+  return q.x + q.y;
 }
 
 // Eight rows of a wavefront straight to LDS (see load_to_lds), four a load, the second four 1 KB on on both sides: the instruction's offset counts for both.
@@ -159,34 +170,45 @@ __device__ __forceinline__ void load_rows_to_lds(u32x4 b, uint32_t lds, uint32_t
                :: "s"(lds), "v"(off), "v"(off2), "s"(b) : "memory", "m0");
 }
 
-// ---- the products of a matrix phase, in order: 16 of the scores S^T = K Q^T of a piece, 16 of O^T += V^T P^T of the one before.  A wavefront issues in order: operand reads go kAhead
-// products ahead.
+// ---- the products of a matrix phase, in order: those of the scores S^T = K Q^T of a piece with 16 operands, those of O^T += V^T P^T of the one before with 16 more, two rows' groups for
+// each.  16 x 16 x 32: with random numbers they and their reads take 1.23 us a piece alone where those of 32 x 32 x 16 take 1.36, for less power (and 1.34 where a wavefront has 64 rows and
+// half the reads); in the whole kernel, where they take twice the issue slots, that is 1 %.  A wavefront issues in order: operand reads go kAhead operands ahead, two at a time.
 constexpr int kAhead = 4;
-__device__ __forceinline__ bf16x8 phase_operand(const KeyAddresses& k, const ValueAddresses& v, int i) {
-  return i < 16 ? lds_read_frag(k[i >> 1] + 32 * (i & 1) * kPieceRow) : value_frag(v, (i - 16) >> 2, (i - 16) & 3);
+__device__ __forceinline__ bf16x8 phase_operand(uint32_t k, uint32_t v, int i) {
+  return i < 16 ? key_operand(k, i >> 2, i & 3) : value_operand(v, (i - 16) >> 3, (i - 16) & 7);
 }
 template <bool kScores>
-__device__ __forceinline__ void first_operands(const KeyAddresses& k, const ValueAddresses& v, bf16x8 (&frag)[kAhead]) {
+__device__ __forceinline__ void first_operands(uint32_t k, uint32_t v, bf16x8 (&frag)[kAhead]) {
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) frag[i] = phase_operand(k, v, (kScores ? 0 : 16) + i);
 }
+// s[m][x][e]: the score of key 16 m + 4 (l / 16) + e with row x of this lane; oacc[db][x][e]: channel 16 db + 4 (l / 16) + e of it
 template <bool kScores, bool kValues, class Beside>
-__device__ __forceinline__ void matrix_phase(const KeyAddresses& k, const ValueAddresses& v, const bf16x8 (&qf)[8], const bf16x8 (&pf)[4], f32x16 (&s)[2],
-                                             f32x16 (&oacc)[4], bf16x8 (&frag)[kAhead], Beside beside) {
+__device__ __forceinline__ void matrix_phase(uint32_t k, uint32_t v, const bf16x8 (&qf)[2][4], const bf16x8 (&pf)[2][2], f32x4 (&s)[4][2], f32x4 (&oacc)[8][2],
+                                             bf16x8 (&frag)[kAhead], Beside beside) {
   constexpr int kFirst = kScores ? 0 : 16, kLast = kValues ? 32 : 16;
   if constexpr (kScores) {
 #pragma unroll
-    for (int mb = 0; mb < 2; ++mb)
+    for (int m = 0; m < 4; ++m)
 #pragma unroll
-      for (int x = 0; x < 16; ++x) s[mb][x] = 0.f;
+      for (int x = 0; x < 2; ++x) s[m][x] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 #pragma unroll
-  for (int i = kFirst; i < kLast; ++i) {
+  for (int i0 = kFirst; i0 < kLast; i0 += 2) {
     __builtin_amdgcn_sched_barrier(0);
-    if (i < 16) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % kAhead], qf[i >> 1], s[i & 1], 0, 0, 0);
-    else oacc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % kAhead], pf[(i - 16) >> 2], oacc[i & 3], 0, 0, 0);
-    if (i + kAhead < kLast) frag[i % kAhead] = phase_operand(k, v, i + kAhead);
-    beside(i);
+#pragma unroll
+    for (int i = i0; i < i0 + 2; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (i < 16) s[i & 3][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag[i % kAhead], qf[x][i >> 2], s[i & 3][x], 0, 0, 0);
+        else oacc[i & 7][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag[i % kAhead], pf[x][(i - 16) >> 3], oacc[i & 7][x], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = i0; i < i0 + 2; ++i) {
+      if (i + kAhead < kLast) frag[i % kAhead] = phase_operand(k, v, i + kAhead);
+      beside(i);
+    }
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -199,7 +221,7 @@ struct Span {
 
 template <bool kE4m3>
 __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
-  const int lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qh = lane >> 5;
+  const int lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = lane >> 4;
   // the same in every lane, and said so: the buffers below are scalar
   W.s = __builtin_amdgcn_readfirstlane(W.s);
   W.t0 = __builtin_amdgcn_readfirstlane(W.t0);
@@ -210,45 +232,50 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
   P.end = __builtin_amdgcn_readfirstlane(P.end);
   const int steps = P.end - P.begin;
   bool wave_on;                    // idle wavefronts still move K and V
-  int first, c_hi, c_lo;           // the first piece; the keys that this lane's row sees
+  int first;                       // the first piece
   int least_hi, most_lo;           // what all rows of the wavefront see: rows are in the order of their tokens, the first one sees the fewest later keys
   float c2;
   const char *k_base, *v_base;
-  f32x16 oacc[4];
-  float ref = -INFINITY, l_run = 0.f;  // see new_reference; the row's sum
+  f32x4 oacc[8][2];
+  float ref, l_run[2];  // see new_reference, of the first or the second row; the rows' sums, of this lane's keys
   auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+    for (int db = 0; db < 8; ++db)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) oacc[db][v] = 0.f;
+      for (int x = 0; x < 2; ++x) oacc[db][x] = f32x4{0.f, 0.f, 0.f, 0.f};
     ref = -INFINITY;
-    l_run = 0.f;
+    l_run[0] = l_run[1] = 0.f;
   };
   clear();
-  bf16x8 qf[8];
+  bf16x8 qf[2][4];
+  auto load_q = [&]() __attribute__((always_inline)) {
+    const Cache& C = arguments().C;
+    const ChunkArgs& A = arguments().A;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const bf16_t* src = (const bf16_t*)A.Q + lane_row(C, A, W, wave, x).row * kD + 8 * (own_lane() >> 4);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) qf[x][s] = *reinterpret_cast<const bf16x8*>(src + 32 * s);
+    }
+  };
+  load_q();
   {
     const Cache& C = arguments().C;
     const ChunkArgs& A = arguments().A;
     const int limit = C.max_pages << C.page_log2, rows = W.nt * C.g;
     first = pieces_of(C, A, W).x + P.begin;
     wave_on = 32 * wave < rows;
-    const LaneRow L = lane_row(C, A, W, wave);
-    c_hi = min(W.place + L.token + 1, limit);
-    c_lo = A.window > 0 ? max(W.place + L.token + 1 - A.window, 0) : 0;
     least_hi = min(W.place + div_g(min(32 * wave, rows - 1), C.g, A.g_magic) + 1, limit);
     most_lo = A.window > 0 ? max(W.place + div_g(min(32 * wave + 31, rows - 1), C.g, A.g_magic) + 1 - A.window, 0) : 0;
     c2 = A.scale * 1.4426950408889634f;
     k_base = C.k;
     v_base = C.v;
-    const bf16_t* src = (const bf16_t*)A.Q + L.row * kD + 8 * qh;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(src + 16 * s);
   }
-  const int v_row = ((lane & 15) >> 2) + 4 * qh;
-  const uint32_t k_at = lds_address(smem) + (lane & 31) * kPieceRow + ((qh ^ row_turn(lane & 31)) << 4);
-  const uint32_t v_at = lds_address(smem + kChunkV) + v_row * kPieceRow + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ row_turn(v_row)) << 4) + 8 * (lane & 1);
-  auto keys = [&](uint32_t off) __attribute__((always_inline)) { return KeyAddresses{k_at + off}; };
-  auto values = [&](uint32_t off) __attribute__((always_inline)) { return ValueAddresses{v_at + off}; };
+  const int v_row = ((lane & 15) >> 2) + 4 * part;
+  const uint32_t k_at = lds_address(smem) + (lane & 15) * kPieceRow + ((part ^ row_turn(lane & 15)) << 4);
+  const uint32_t v_at = lds_address(smem + kChunkV) + v_row * kPieceRow + ((((lane & 3) >> 1) ^ row_turn(v_row)) << 4) + 8 * (lane & 1);
+  auto keys = [&](uint32_t off) __attribute__((always_inline)) { return k_at + off; };
+  auto values = [&](uint32_t off) __attribute__((always_inline)) { return v_at + off; };
 
   // ---- pages: lane l knows those of piece base + l of the span, whose four 16-token groups may each have another one; this wavefront moves rows 8 wave.. of a piece
   constexpr int kRow = kE4m3 ? kD : kPieceRow;
@@ -300,16 +327,20 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
     const uint64_t at = (uint64_t)m.from(base);
     load_rows_to_lds(u32x4{(uint32_t)at, (uint32_t)(at >> 32), m.bytes(), 0x00020000u}, lds_rows + lds_off, move_off, move_off2);
   };
-  // e4m3: one load of eight rows into registers, to be written to LDS as bf16
+  // e4m3: eight rows into registers, to be written to LDS as bf16; eight lanes have a row, each eight channels of its lower half and eight of its upper one, so that what they write at
+  // once lies in different banks (sixteen channels of a row: 1890 us where this takes 1867)
+  const uint32_t fetch_off = (lane >> 3) * kD + (lane & 7) * 8;
   auto fetch = [&](const char* base, const Move& m) __attribute__((always_inline)) {
-    return __builtin_amdgcn_raw_buffer_load_b128(buffer_of(m.from(base), m.bytes()), lane * 16, 0, 0);
+    const auto rows = buffer_of(m.from(base), m.bytes());
+    const auto lo = __builtin_amdgcn_raw_buffer_load_b64(rows, fetch_off, 0, 0), hi = __builtin_amdgcn_raw_buffer_load_b64(rows, fetch_off + kD / 2, 0, 0);
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
   };
   const int put_row = 8 * wave + (lane >> 3);
-  const uint32_t put_at = lds_address(smem) + put_row * kPieceRow + (((2 * (lane & 7)) ^ row_turn(put_row)) << 4);
+  const uint32_t put_at = lds_address(smem) + put_row * kPieceRow + (((lane & 7) ^ row_turn(put_row)) << 4);
   auto put = [&](u32x4 x, float scale, uint32_t lds_off) __attribute__((always_inline)) {
     const uint32_t at = put_at + lds_off;
     lds_write_16(at, eight_bf16(x[0], x[1], scale));
-    lds_write_16(at ^ 16, eight_bf16(x[2], x[3], scale));
+    lds_write_16(at ^ 128, eight_bf16(x[2], x[3], scale));
   };
   // a tile of K or V at once, in front of the main loop and in the simple one
   auto stage = [&](const char* base, const Move& m, float scale, uint32_t lds_off) __attribute__((always_inline)) {
@@ -317,45 +348,65 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
     else move(base, m, lds_off);
   };
 
-  // Scores -> what their exponents are taken against: keys that this lane's row does not see become -inf, the row's maximum joins the running one.
-  float alpha, mc;
-  auto reference = [&](int step, uint32_t word, float slack, f32x16 (&s)[2]) __attribute__((always_inline)) {
+  // Scores -> what their exponents are taken against: keys that a row does not see become -inf, the row's maximum joins the running one.
+  float alpha;
+  Two mc;
+  auto reference = [&](int step, uint32_t word, float slack, f32x4 (&s)[4][2]) __attribute__((always_inline)) {
     if (!(word & 16)) {
-      const int key0 = (first + step) * 64, lim = c_hi - key0 - 4 * qh, lo = c_lo - key0 - 4 * qh;
+      const Cache& C = arguments().C;
+      const int limit = C.max_pages << C.page_log2, window = arguments().A.window, key0 = (first + step) * 64 + 4 * (own_lane() >> 4);
 #pragma unroll
-      for (int mb = 0; mb < 2; ++mb)
+      for (int x = 0; x < 2; ++x) {
+        const int upto = W.place + lane_row(C, arguments().A, W, wave, x).token + 1;
+        const int lim = min(upto, limit) - key0, lo = (window > 0 ? max(upto - window, 0) : 0) - key0;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int key = 32 * mb + 8 * (v >> 2) + (v & 3);  // and 4 qh
-          const bool shown = word >> (2 * mb + (v >> 3)) & 1;
-          if (key >= (shown ? lim : 0) || key < lo) s[mb][v] = -INFINITY;
+        for (int m = 0; m < 4; ++m) {
+          const bool shown = word >> m & 1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (16 * m + e >= (shown ? lim : INT32_MIN) || 16 * m + e < lo) s[m][x][e] = -INFINITY;
         }
-    }
-    float m[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      m[x] = fmaxf(s[x >> 1][8 * (x & 1)], s[x >> 1][8 * (x & 1) + 1]);
-#pragma unroll
-      for (int v = 2; v < 8; v += 2) m[x] = fmaxf(fmaxf(m[x], s[x >> 1][8 * (x & 1) + v]), s[x >> 1][8 * (x & 1) + v + 1]);
-    }
-    mc = new_reference(both_halves_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * c2, ref, alpha, slack);
-  };
-  // Scores -> probabilities as the operands of the four contraction steps of P V; l_run is of this lane's keys.
-  auto probabilities = [&](const f32x16 (&s)[2], bf16x8 (&pf)[4]) __attribute__((always_inline)) {
-    float l[2] = {0.f, 0.f};
-#pragma unroll
-    for (int sp = 0; sp < 4; ++sp)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[sp >> 1][8 * (sp & 1) + e], c2, -mc));
-        l[e & 1] += p;
-        pf[sp][e] = (bf16_t)p;
       }
-    l_run = fmaf(l_run, alpha, l[0] + l[1]);
-    // Along a sequence maxima soon stop growing: the sums are rescaled where one of the wavefront's rows has a new one
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0ull) {
+    }
+    float most[2];
 #pragma unroll
-      for (int db = 0; db < 4; ++db) oacc[db] *= alpha;
+    for (int x = 0; x < 2; ++x) {
+      float m[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        m[h] = fmaxf(fmaxf(s[2 * h][x][0], s[2 * h][x][1]), s[2 * h][x][2]);
+        m[h] = fmaxf(fmaxf(m[h], s[2 * h][x][3]), s[2 * h + 1][x][0]);
+        m[h] = fmaxf(fmaxf(m[h], s[2 * h + 1][x][1]), s[2 * h + 1][x][2]);
+      }
+      most[x] = fmaxf(fmaxf(m[0], s[1][x][3]), fmaxf(m[1], s[3][x][3]));
+    }
+    mc = both_rows(new_reference(row_max(most[0], most[1]) * c2, ref, alpha, slack));
+  };
+  // Scores -> probabilities as the operands of the two contraction steps of P V.
+  auto probabilities = [&](const f32x4 (&s)[4][2], bf16x8 (&pf)[2][2]) __attribute__((always_inline)) {
+    // Along a sequence maxima soon stop growing: the sums are rescaled where one of the wavefront's rows has a new reference
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0ull) {
+      const Two by = both_rows(alpha);
+      l_run[0] *= by.x;
+      l_run[1] *= by.y;
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        oacc[db][0] *= by.x;
+        oacc[db][1] *= by.y;
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      float l[2] = {0.f, 0.f};
+#pragma unroll
+      for (int sp = 0; sp < 2; ++sp)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[2 * sp + (e >> 2)][x][e & 3], c2, -(x ? mc.y : mc.x)));
+          l[e & 1] += p;
+          pf[x][sp][e] = (bf16_t)p;
+        }
+      l_run[x] += l[0] + l[1];
     }
   };
 
@@ -370,11 +421,11 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
-    f32x16 s[2];
-    bf16x8 pf[4], frag[kAhead];
+    f32x4 s[4][2];
+    bf16x8 pf[2][2], frag[kAhead];
     u32x4 kr, vr;  // e4m3: on the way to LDS
     look_up(0);
-    await_rows(qf);
+    asm volatile("" : "+v"(qf[0][0]), "+v"(qf[0][1]), "+v"(qf[0][2]), "+v"(qf[0][3]), "+v"(qf[1][0]), "+v"(qf[1][1]), "+v"(qf[1][2]), "+v"(qf[1][3]));  // (waited for here, not in the loop)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const Move m = move_of(i);
@@ -461,9 +512,11 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
     // keys as zeros.
     float mark = 0.f;
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+    for (int db = 0; db < 8; ++db)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) mark = fmaf(oacc[db][v], 0.f, mark);
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mark = fmaf(oacc[db][x][e], 0.f, mark);
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem);
     const bool marked = __builtin_amdgcn_ballot_w64(wave_on && mark != 0.f) != 0ull;
     if (lane == 0) marks[wave] = marked;
@@ -477,11 +530,12 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
       const Cache& C = arguments().C;
       const ChunkArgs& A = arguments().A;
       const int limit = C.max_pages << C.page_log2, rows = W.nt * C.g, window = A.window;
-      const int token = lane_row(C, A, W, wave).token;
+      const int token[2] = {lane_row(C, A, W, wave, 0).token, lane_row(C, A, W, wave, 1).token};
       const int t_first = div_g(32 * wave, C.g, A.g_magic), t_last = div_g(min(32 * wave + 31, rows - 1), C.g, A.g_magic);
 #pragma unroll 1
       for (int step = 0; step < steps; ++step) {
         if (step == 0 || step - base == 64) look_up(step);
+        load_q();  // (not kept: the registers are what this loop is short of)
         const Move a = move_of(step);
         stage(k_base, a, a.ks(), 0);
         stage(v_base, a, a.vs(), kChunkV);
@@ -498,27 +552,27 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
             matrix_phase<false, true>(keys(0), values(0), qf, pf, s, oacc, frag, nothing);
           } else {
 #pragma unroll
-            for (int sp = 0; sp < 4; ++sp) {
+            for (int sp = 0; sp < 2; ++sp) {
 #pragma unroll 1
               for (int k = t_first; k <= t_last; ++k) {
                 const int k_hi = min(W.place + k + 1, limit) - key0, k_lo = (window > 0 ? max(W.place + k + 1 - window, 0) : 0) - key0;
 #pragma unroll
-                for (int db = 0; db < 4; ++db) {
+                for (int db = 0; db < 8; ++db) {
                   __builtin_amdgcn_sched_barrier(0);  // one product's operands at a time
-                  ValueAddresses at = values(0);
-                  asm volatile("" : "+v"(at.at));
-                  bf16x8 x = value_frag(at, sp, db);
+                  uint32_t at = values(0);
+                  asm volatile("" : "+v"(at));
+                  bf16x8 v = value_operand(at, sp, db);
 #pragma unroll
                   for (int e = 0; e < 8; ++e) {
-                    const int key = 16 * sp + 8 * (e >> 2) + (e & 3);  // and 4 qh
-                    if (4 * qh < k_lo - key || 4 * qh >= k_hi - key) x[e] = (bf16_t)0.f;
+                    const int key = 32 * sp + 16 * (e >> 2) + (e & 3);  // and 4 part
+                    if (4 * part < k_lo - key || 4 * part >= k_hi - key) v[e] = (bf16_t)0.f;
                   }
-                  f32x16 add;
 #pragma unroll
-                  for (int v = 0; v < 16; ++v) add[v] = 0.f;
-                  add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[sp], add, 0, 0, 0);
+                  for (int x = 0; x < 2; ++x) {
+                    const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[x][sp], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-                  for (int v = 0; v < 16; ++v) oacc[db][v] += token == k ? add[v] : 0.f;
+                    for (int e = 0; e < 4; ++e) oacc[db][x][e] += token[x] == k ? add[e] : 0.f;
+                  }
                 }
               }
             }
@@ -528,56 +582,56 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
       }
     }
   }
-  l_run += __shfl_xor(l_run, 32);
+  const float l_all = row_sum(l_run[0], l_run[1]);  // of the first or the second row, as ref
 
   const Cache& C = arguments().C;
   const ChunkArgs& A = arguments().A;
   const int rows = W.nt * C.g;
   if (!wave_on) return;
-  const LaneRow L = lane_row(C, A, W, wave);
-  const int lane_b = own_lane(), col = lane_b & 31, half = lane_b >> 5;
+  const int lane_b = own_lane(), col = lane_b & 15, quarter = lane_b >> 4;
   if (!P.whole) {
-    {
-      f32x4* to = reinterpret_cast<f32x4*>(A.part) + ((int64_t)P.slot * kChunkWaves + wave) * 1024 + lane_b;
+    f32x4* to = reinterpret_cast<f32x4*>(A.part) + ((int64_t)P.slot * kChunkWaves + wave) * 1024 + lane_b;
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
+    for (int db = 0; db < 8; ++db)
 #pragma unroll
-        for (int a = 0; a < 4; ++a) to[64 * (4 * db + a)] = f32x4{oacc[db][4 * a], oacc[db][4 * a + 1], oacc[db][4 * a + 2], oacc[db][4 * a + 3]};
-      if (half == 0) A.part_ml[(int64_t)P.slot * kChunkRows + L.r] = float2{ref, l_run};
-    }
+      for (int x = 0; x < 2; ++x) to[64 * (2 * db + x)] = oacc[db][x];
+    if ((quarter & 1) == 0) A.part_ml[(int64_t)P.slot * kChunkRows + 32 * wave + 16 * (quarter >> 1) + col] = float2{ref, l_all};
     return;
   }
-  const bool some = l_run > 0.f || l_run != l_run;
-  const float inv = 1.f / l_run;
-  float gate = 0.f;
-  uint2 acc[16];
-#pragma unroll
-  for (int x = 0; x < 16; ++x) acc[x] = uint2{0u, 0u};
-  if (A.gate && L.here) {
-    gate = A.gate[L.row];
-    if (A.o_acc) {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) acc[x] = *reinterpret_cast<const uint2*>((const bf16_t*)A.o_acc + L.row * kD + 8 * x + 4 * half);
-    }
-  }
+  const Two total = both_rows(l_all);
   char* own = smem + 32 * wave * kPieceRow;
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+  for (int x = 0; x < 2; ++x) {
+    const LaneRow L = lane_row(C, A, W, wave, x);
+    const float l = x ? total.y : total.x, inv = 1.f / l;
+    const bool some = l > 0.f || l != l;
+    float gate = 0.f;
+    uint2 acc[8];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
+    for (int db = 0; db < 8; ++db) acc[db] = uint2{0u, 0u};
+    if (A.gate && L.here) {
+      gate = A.gate[L.row];
+      if (A.o_acc) {
+#pragma unroll
+        for (int db = 0; db < 8; ++db) acc[db] = *reinterpret_cast<const uint2*>((const bf16_t*)A.o_acc + L.row * kD + 16 * db + 4 * quarter);
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
       float o[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = some ? oacc[db][4 * a + e] * inv : 0.f;  // an empty row is 0 whatever its values are
+      for (int e = 0; e < 4; ++e) o[e] = some ? oacc[db][x][e] * inv : 0.f;  // an empty row is 0 whatever its values are
       if (A.gate) {
-        const uint2 x = acc[4 * db + a];
-        o[0] = fmaf(gate, o[0], bf16_lo(x.x));
-        o[1] = fmaf(gate, o[1], bf16_hi(x.x));
-        o[2] = fmaf(gate, o[2], bf16_lo(x.y));
-        o[3] = fmaf(gate, o[3], bf16_hi(x.y));
+        o[0] = fmaf(gate, o[0], bf16_lo(acc[db].x));
+        o[1] = fmaf(gate, o[1], bf16_hi(acc[db].x));
+        o[2] = fmaf(gate, o[2], bf16_lo(acc[db].y));
+        o[3] = fmaf(gate, o[3], bf16_hi(acc[db].y));
       }
-      *reinterpret_cast<uint2*>(own + col * kPieceRow + (((4 * db + a) ^ (col & 15)) << 4) + 8 * half) = uint2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+      *reinterpret_cast<uint2*>(own + (16 * x + col) * kPieceRow + (((2 * db + (quarter >> 1)) ^ col) << 4) + 8 * (quarter & 1)) = uint2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
     }
-  if (half == 0 && L.here) A.LSE[L.row] = some ? (finite_reference(ref) + __builtin_amdgcn_logf(l_run)) * 0.6931471805599453f : -INFINITY;
+    const float at = x ? both_rows(ref).y : both_rows(ref).x;
+    if (quarter == 0 && L.here) A.LSE[L.row] = some ? (finite_reference(at) + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+  }
   wave_sync();
   const int sub = lane_b & 15;
 #pragma unroll
@@ -741,27 +795,48 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
 __global__ void __launch_bounds__(kChunkJoinThreads) k_cache_chunk_join(Args X) {
   const Cache& C = X.C;
   const ChunkArgs& A = X.A;
-  __shared__ __align__(16) char smem[4 * 18 * 64 * 4];
+  __shared__ __align__(16) char smem[4 * 5 * 64 * 16];
   constexpr int kBatch = 4;
   const int b = (int)(blockIdx.x >> 3), rw = (int)(blockIdx.x & 7);
   const Joint J = A.joints[b];
   const int rows = J.nt * C.g, n = J.parts;
   if (n == 0 || 32 * rw >= rows) return;
-  const int lane = threadIdx.x & 63, db = threadIdx.x >> 6 & 3, half = threadIdx.x >> 8, col = lane & 31, qh = lane >> 5;
-  const int r = 32 * rw + col, rc = min(r, rows - 1), tt = div_g(rc, C.g, A.g_magic), hh = rc - tt * C.g;
-  float top = -INFINITY, total = 0.f;
+  const int lane = threadIdx.x & 63, db = threadIdx.x >> 6 & 3, half = threadIdx.x >> 8, col = lane & 15, quarter = lane >> 4;
+  // this lane's rows col and 16 + col; o[2 h + x]: channels 32 db + 16 h + 4 quarter .. of row x
+  int64_t row[2];
+  bool here[2];
+  int rc[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int r = 32 * rw + 16 * x + col;
+    here[x] = r < rows;
+    rc[x] = min(r, rows - 1);
+    const int tt = div_g(rc[x], C.g, A.g_magic);
+    row[x] = (int64_t)(J.t0 + tt) * C.hq + J.j * C.g + rc[x] - tt * C.g;
+  }
+  float top[2] = {-INFINITY, -INFINITY}, total[2] = {0.f, 0.f};
   f32x4 o[4];
 #pragma unroll
   for (int a = 0; a < 4; ++a) o[a] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto add = [&](int x, float ref, float sum, const f32x4& first, const f32x4& second) __attribute__((always_inline)) {
+    float f0;
+    const float mc = new_reference(ref, top[x], f0, 0.f), f1 = __builtin_amdgcn_exp2f(ref - mc);
+    total[x] = fmaf(total[x], f0, f1 * sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[x][e] = fmaf(o[x][e], f0, f1 * first[e]);
+      o[2 + x][e] = fmaf(o[2 + x][e], f0, f1 * second[e]);
+    }
+  };
   for (int i0 = half; i0 < n; i0 += 2 * kBatch) {
-    float2 x[kBatch];
+    float2 ml[kBatch][2];
     f32x4 y[kBatch][4];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int i = min(i0 + 2 * k, n - 1);
       const int64_t at = min(i == 0 ? J.first : J.second + 2 * (i - 1), 2 * kSlots - 1);  // (less in any case, unless starts are not in order)
-      x[k] = A.part_ml[at * kChunkRows + rc];
-      if (i0 + 2 * k >= n) x[k] = float2{-INFINITY, 0.f};
+#pragma unroll
+      for (int x = 0; x < 2; ++x) ml[k][x] = A.part_ml[at * kChunkRows + rc[x]];
       const f32x4* from = reinterpret_cast<const f32x4*>(A.part) + (at * kChunkWaves + rw) * 1024 + 256 * db + lane;
 #pragma unroll
       for (int a = 0; a < 4; ++a) y[k][a] = from[64 * a];
@@ -769,56 +844,48 @@ __global__ void __launch_bounds__(kChunkJoinThreads) k_cache_chunk_join(Args X) 
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       if (i0 + 2 * k >= n) break;
-      float f0;
-      const float mc = new_reference(x[k].x, top, f0, 0.f), f1 = __builtin_amdgcn_exp2f(x[k].x - mc);
-      total = fmaf(total, f0, f1 * x[k].y);
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[a][e] = fmaf(o[a][e], f0, f1 * y[k][a][e]);
+      for (int x = 0; x < 2; ++x) add(x, ml[k][x].x, ml[k][x].y, y[k][x], y[k][2 + x]);
     }
   }
-  float* hand = reinterpret_cast<float*>(smem) + db * 18 * 64 + lane;
+  f32x4* hand = reinterpret_cast<f32x4*>(smem) + db * 5 * 64 + lane;
   if (half == 1) {
-    hand[0] = top;
-    hand[64] = total;
+    hand[0] = f32x4{top[0], total[0], top[1], total[1]};
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) hand[64 * (2 + 4 * a + e)] = o[a][e];
+    for (int a = 0; a < 4; ++a) hand[64 * (1 + a)] = o[a];
   }
   __syncthreads();
   if (half == 0) {
-    float f0;
-    const float his = hand[0], mc = new_reference(his, top, f0, 0.f), f1 = __builtin_amdgcn_exp2f(his - mc);
-    total = fmaf(total, f0, f1 * hand[64]);
+    const f32x4 his = hand[0];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[a][e] = fmaf(o[a][e], f0, f1 * hand[64 * (2 + 4 * a + e)]);
+    for (int x = 0; x < 2; ++x) add(x, his[2 * x], his[2 * x + 1], hand[64 * (1 + x)], hand[64 * (3 + x)]);
   }
   __syncthreads();
   if (half == 0) {
-    const bool some = total > 0.f || total != total, here = r < rows;
-    const float inv = 1.f / total;
-    const int64_t row = (int64_t)(J.t0 + tt) * C.hq + J.j * C.g + hh;
-    float gate = 0.f;
-    if (A.gate && here) gate = A.gate[row];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
+    for (int x = 0; x < 2; ++x) {
+      const bool some = total[x] > 0.f || total[x] != total[x];
+      const float inv = 1.f / total[x];
+      float gate = 0.f;
+      if (A.gate && here[x]) gate = A.gate[row[x]];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[a][e] = some ? o[a][e] * inv : 0.f;
-      if (A.gate) {
-        uint2 x = {0u, 0u};
-        if (A.o_acc && here) x = *reinterpret_cast<const uint2*>((const bf16_t*)A.o_acc + row * kD + 32 * db + 8 * a + 4 * qh);
-        o[a][0] = fmaf(gate, o[a][0], bf16_lo(x.x));
-        o[a][1] = fmaf(gate, o[a][1], bf16_hi(x.x));
-        o[a][2] = fmaf(gate, o[a][2], bf16_lo(x.y));
-        o[a][3] = fmaf(gate, o[a][3], bf16_hi(x.y));
+      for (int h = 0; h < 2; ++h) {
+        f32x4 y = o[2 * h + x];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = some ? y[e] * inv : 0.f;
+        if (A.gate) {
+          uint2 z = {0u, 0u};
+          if (A.o_acc && here[x]) z = *reinterpret_cast<const uint2*>((const bf16_t*)A.o_acc + row[x] * kD + 32 * db + 16 * h + 4 * quarter);
+          y[0] = fmaf(gate, y[0], bf16_lo(z.x));
+          y[1] = fmaf(gate, y[1], bf16_hi(z.x));
+          y[2] = fmaf(gate, y[2], bf16_lo(z.y));
+          y[3] = fmaf(gate, y[3], bf16_hi(z.y));
+        }
+        *reinterpret_cast<uint2*>(smem + (16 * x + col) * kPieceRow + (((4 * db + 2 * h + (quarter >> 1)) ^ col) << 4) + 8 * (quarter & 1)) =
+            uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
       }
-      *reinterpret_cast<uint2*>(smem + col * kPieceRow + (((4 * db + a) ^ (col & 15)) << 4) + 8 * qh) = uint2{pack_bf16x2(o[a][0], o[a][1]), pack_bf16x2(o[a][2], o[a][3])};
+      if (db == 0 && quarter == 0 && here[x]) A.LSE[row[x]] = some ? (finite_reference(top[x]) + __builtin_amdgcn_logf(total[x])) * 0.6931471805599453f : -INFINITY;
     }
-    if (db == 0 && qh == 0 && here) A.LSE[row] = some ? (finite_reference(top) + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
   }
   __syncthreads();
   const int sub = threadIdx.x & 15, wr = (int)(threadIdx.x >> 4), rr = 32 * rw + wr;

@@ -90,9 +90,7 @@ __device__ __forceinline__ bf16x8 piece_probabilities(const f32x16 (&sacc)[2], i
   return pf;
 }
 
-// VAddr: the addresses as piece_addresses gives them, or what makes them when they are asked for.
-template <class VAddr>
-__device__ __forceinline__ bf16x8 value_frag(const VAddr& vaddr, int sp, int db) {
+__device__ __forceinline__ bf16x8 value_frag(const uint32_t (&vaddr)[2][4], int sp, int db) {
   const bf16x4 a0 = lds_read_tr_at(vaddr[0][db] + 16 * sp * kPieceRow), a1 = lds_read_tr_at(vaddr[1][db] + 16 * sp * kPieceRow);
   return __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
 }

@@ -68,20 +68,9 @@ def test_a_wait_state_follows_every_write_of_m0(code):
     assert loads >= 22                                             # two a tile: seven tiles in front of the loop, two in it, two where values are not finite
 
 
-def test_small_kernels_keep_everything_in_registers(code):
-    for source in ("rotary", "cache_read"):
-        spills = re.findall(r"\.name:\s+(_ZN3nsa\S+)\n(?:.*\n)*?\s+\.vgpr_spill_count:\s+(\d+)", code[source])
-        scratch = re.findall(r"\.name:\s+(_ZN3nsa\S+)\n\s+\.private_segment_fixed_size:\s+(\d+)", code[source])
-        assert spills and [n for _, n in spills + scratch if n != "0"] == []
-
-
-def test_the_loop_over_the_pieces_touches_no_scratch(code):
-    """A reload in the loop would wait for the keys and values that are on their way to LDS: what does not fit in registers lies in front of and behind it."""
-    for form in ("ILb0EE", "ILb1EE"):
-        start = code["cache_chunk"].index("\n_ZN3nsa12_GLOBAL__N_118k_cache_chunk_even" + form)
-        text = code["cache_chunk"][start:code["cache_chunk"].index(".end_amdhsa_kernel", start)]
-        parts = re.split(r"^\s+s_barrier$", text, flags=re.M)
-        matrix = [i for i, p in enumerate(parts) if p.count("v_mfma") == 32]
-        assert len(matrix) == 1, matrix                             # the matrix phase, and behind its barrier the vector phase
-        assert "scratch_" not in parts[matrix[0]] and "scratch_" not in parts[matrix[0] + 1]
-        assert parts[matrix[0] + 1].count("v_exp_f32") == 33
+@pytest.mark.parametrize("source,kernels", [("rotary", 1), ("cache_read", 2), ("cache_chunk", 3)])
+def test_everything_is_kept_in_registers(code, source, kernels):
+    """A reload in the loop over the pieces would wait for the keys and values that are on their way to LDS."""
+    spills = re.findall(r"\.name:\s+(_ZN3nsa\S+)\n(?:.*\n)*?\s+\.vgpr_spill_count:\s+(\d+)", code[source])
+    scratch = re.findall(r"\.name:\s+(_ZN3nsa\S+)\n\s+\.private_segment_fixed_size:\s+(\d+)", code[source])
+    assert len(spills) == len(scratch) == kernels and [n for _, n in spills + scratch if n != "0"] == []
