@@ -5,9 +5,9 @@
 // SIMD, each with its Q and its output in registers, share a piece's K and V in LDS.  A piece is 32 KB and 8.4 MFLOP, 2048 clocks of the matrix pipes; reading its operands takes the
 // LDS as long.
 //
-// What bounds it is power and the vector phase before the pipes: with random numbers the products of a piece and their operand reads alone take 1.23 us, at 1.7 GHz; with moving K and V
-// and the softmax it is 1.68 at 2.1 GHz, 3570 clocks, of which a wavefront's vector phase is 1760 and its matrix phase 1500, beside another's vector phase.  A large library product reaches 1.6
-// PFLOP/s; 2048 new tokens of 32 heads behind 32768 keys (8 KV heads) take 0.94 to 0.99 ms, 1.15 to 1.2 PFLOP/s.
+// What bounds it is the vector phase, and power: a wavefront's vector phase takes 1760 clocks, its matrix phase, beside another's vector phase, 1500, both together 3570, at 2.0 to 2.1 GHz
+// with random numbers.  (The products of a piece and their operand reads alone: 1.23 us, at 1.7 GHz; the whole: 1.68.)  2048 new tokens of 32 heads behind 32768 keys (8 KV heads) take 0.94 to
+// 1.0 ms by card, 1.13 to 1.2 PFLOP/s; a large library product reaches 1.6.
 //
 // A page of 16 tokens or more is a run of memory, so the eight rows that a wavefront moves of a piece's K and V are always one page's: which one is looked up for 64 pieces
 // at a time, a piece a lane.
