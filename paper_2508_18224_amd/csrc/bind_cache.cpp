@@ -660,6 +660,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Turn how = {dims(a[2], "inv_freq", 1), maybe(a[3], "cu_seqlens", 1), maybe(a[4], "positions", 1), truth(a[5]), truth(a[7]), PyFloat_AsDouble(a[6]), PyLong_AsVoidPtr(a[11])};
     if (PyErr_Occurred()) throw python_error();
     if (truth(a[10])) {
+      if (how.inv_freq.requires_grad()) throw Refused{"inv_freq requires grad, and the rotation has a gradient for q and k only: detach it"};
       without_gil([&] {
         auto r = Rotation::of(x[0], x[1], how);
         for (size_t i = 0; i < r.size(); ++i) y[i] = std::move(r[i]);

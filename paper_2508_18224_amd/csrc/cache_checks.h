@@ -57,6 +57,9 @@ inline int check_cache_pointers(const nsa_sel_cache_shape* s, const void* k, con
   return NSA_SEL_OK;
 }
 
+// Lengths below this one are this one: places that follow from them are negative all the same, and no sum leaves 32 bits.
+constexpr int kLeastLength = -(1 << 30);
+
 // No place is as far back as 2^30 of another: a window that long is none, and the kernels' sums with one stay in 32 bits.
 inline int32_t window_of(const nsa_sel_cache_shape* s) { return s->window < (1 << 30) ? s->window : 0; }
 

@@ -82,7 +82,7 @@ __device__ __forceinline__ Unit unit_of(const Cache& C, const ChunkArgs& A, int 
   W.j = j;
   W.t0 = c0 + i0;
   W.nt = min(min(A.tok, n - i0), C.T - W.t0);
-  W.place = C.kv_len[s] - n + i0;
+  W.place = max(C.kv_len[s], kLeastLength) - n + i0;
   if (W.nt <= 0 || W.t0 < 0) W.s = -1;
   return W;
 }

@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(kReadThreads) k_cache_read(Cache C, ReadArgs A
     int s = t, place = -1;
     bool on = threadIdx.x < kReadTokens && t < C.T;
     if (C.cu == nullptr) {
-      if (on) place = C.kv_len[t] - 1;
+      if (on) place = max(C.kv_len[t], kLeastLength) - 1;
     } else {
       // The first token's sequence, by all lanes; the others are in it too, or found by a search of their own.  Tokens of no sequence are before the first one's or
       // after the last one's.
@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(kReadThreads) k_cache_read(Cache C, ReadArgs A
         }
         s = lo;
       }
-      if (on) place = C.kv_len[s] - C.cu[s + 1] + t;
+      if (on) place = max(C.kv_len[s], kLeastLength) - C.cu[s + 1] + t;
     }
     if (threadIdx.x < kReadTokens) where[threadIdx.x] = int2{on ? page_of(C, s, place) : -2, place & ((1 << C.page_log2) - 1)};
   }

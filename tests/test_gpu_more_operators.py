@@ -315,6 +315,22 @@ def test_largest_values():
         check_chunks(o[rows], lse[rows], tuple(x[rows] for x in ref), keys=700, most=most)
 
 
+def test_lengths_of_any_sign():
+    """The least length that a number of 32 bits holds is a negative one like others: nothing is seen, rows are zero."""
+    b = Batch(175, [70, 300, 40], hq=8, hkv=2, page=32)
+    cache = b.upload(nsa)
+    b.dlen[0], b.dlen[2] = -2 ** 31, -2 ** 31 + 5
+    o, lse = cache.attention_chunk(b.dq, b.dtable, b.dlen)
+    k, v = cache.read(b.dtable, b.dlen)
+    for i in (0, 2):
+        assert (o[i] == 0).all() and torch.isneginf(lse[i]).all() and (k[i] == 0).all() and (v[i] == 0).all()
+    assert torch.isfinite(lse[1]).all() and (k[1] != 0).any()
+    far = torch.full_like(b.dlen, 2 ** 31 - 1)                           # past the table: what it holds is seen, a place without a page is zero
+    o, lse = cache.attention_chunk(b.dq, b.dtable, far, window=5)
+    assert (o == 0).all() and torch.isneginf(lse).all()
+    assert (cache.read(b.dtable, far)[0] == 0).all()
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_results_in_place_of_the_sum_so_far(e4m3):
     """out may be o_acc: units that one workgroup has, and such as are joined from parts."""

@@ -162,6 +162,9 @@ def test_python_rotary():
             nsa.rotary(**args)
     with pytest.raises(nsa.NsaSelError, match="requires grad"):                       # a result that is given takes no gradient
         nsa.rotary(**_with(ok, q=q.clone().requires_grad_(), q_out=q.clone()))
+    for grad in (q.clone().requires_grad_(), q):                                      # frequencies have no gradient
+        with pytest.raises(nsa.NsaSelError, match="inv_freq requires grad"):
+            nsa.rotary(**_with(ok, q=grad, inv_freq=f.clone().requires_grad_()))
 
 
 def test_frequencies():
