@@ -25,7 +25,7 @@ namespace {
 constexpr int kChunkWaves = 8, kChunkRows = 32 * kChunkWaves, kChunkThreads = 64 * kChunkWaves;
 constexpr int kStages = 4;  // tiles of K, and of V: one more than a piece that is asked for two before it is used needs, so that nobody waits for the tile to be free
 constexpr int kChunkV = kStages * kPieceBytes, kChunkLds = 2 * kStages * kPieceBytes + 64;
-constexpr int kSlots = 256;  // workgroups that share all units' pieces evenly
+constexpr int kSlots = 256;  // workgroups that share all units' pieces evenly, at most
 // What a unit costs beside its pieces, in pieces: its Q, its pages, the first and the last piece, its result, 10 to 12 us for 1.9 of a piece.  (A whole prompt of 8192 tokens: 1300 us
 // with none of it counted, 1023 with 5, 1004 with 6, 1013 with 8.)
 constexpr int kUnitCost = 6;
@@ -44,6 +44,7 @@ struct ChunkArgs {
   int32_t tok;       // tokens of a unit
   uint32_t g_magic;  // see div_g
   int32_t units;     // of a KV head, at most
+  int32_t slots;     // workgroups, a multiple of 8
   // parts of units: slot 2 w of workgroup w for the unit that others begin, 2 w + 1 for the one that it begins and others finish
   float* part;       // [slots][8 wavefronts][16][64 lanes][4]: the sums as the lanes hold them
   float2* part_ml;   // [slots][256] (reference, sum)
@@ -655,7 +656,7 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
   }
 }
 
-// All units' pieces cut into kSlots equal parts, one after the other, so that all workgroups end together whatever the lengths, which only the device knows.  A workgroup
+// All units' pieces cut into equal parts, one for each workgroup, one after the other, so that all workgroups end together whatever the lengths, which only the device knows.  A workgroup
 // finds its first unit by a scan over those of a head.
 __device__ __forceinline__ int64_t uniform(int64_t x) {  // a value that all lanes have, in scalar registers
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
@@ -674,7 +675,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
   const ChunkArgs& A = arguments().A;
   extern __shared__ __align__(256) char smem[];
   // XCDs get workgroups in turn, and take an eighth of all pieces each: with eight KV heads one head's, which its L2 then serves
-  const int wg = (int)(blockIdx.x & 7) * (kSlots / 8) + (int)(blockIdx.x >> 3);
+  const int wg = (int)(blockIdx.x & 7) * (A.slots >> 3) + (int)(blockIdx.x >> 3);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (A.units + kChunkThreads - 1) / kChunkThreads, u0 = threadIdx.x * per, u1 = min(u0 + per, A.units);
   // of the units u0 .. u1 - 1 of a head, `visit` those that there are with their cost
@@ -723,7 +724,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
     of_head += sums[w];
   }
   of_head = uniform(of_head);
-  const int64_t total = of_head * C.hkv, share = max((total + kSlots - 1) / kSlots, (int64_t)kLeastShare), start = wg * share;
+  const int64_t total = of_head * C.hkv, share = max((total + A.slots - 1) / A.slots, (int64_t)kLeastShare), start = wg * share;
   if (threadIdx.x == 0) A.joints[wg].parts = 0;
   if (start >= total) return;  // the whole workgroup
   const int j = total < (int64_t)1 << 32 ? (int)((uint32_t)start / (uint32_t)of_head) : (int)(start / of_head);
@@ -754,7 +755,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) k_cache_chunk_even(Args) {
       const int64_t q = uniform(state->q), left = uniform(state->left);
       const int n = pieces_of(C, A, W).y;
       const int64_t cost = kUnitCost + n, begin = cut_at(q, cost), end = q + left >= cost ? cost : cut_at(q + left, cost);
-      const int wg = (int)(blockIdx.x & 7) * (kSlots / 8) + (int)(blockIdx.x >> 3);
+      const int wg = (int)(blockIdx.x & 7) * (A.slots >> 3) + (int)(blockIdx.x >> 3);
       Span P;
       P.begin = max((int)begin - kUnitCost, 0);
       P.end = max((int)end - kUnitCost, 0);
@@ -908,7 +909,7 @@ __global__ void __launch_bounds__(kChunkJoinThreads) k_cache_chunk_join(Args X) 
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------------
 struct ChunkCut {
-  int tok;
+  int tok, slots;
   int64_t units;
   size_t ml, joints, total;  // offsets in the workspace; the sums come first
 };
@@ -916,6 +917,11 @@ ChunkCut chunk_cut(const nsa_sel_cache_shape* s) {
   ChunkCut c;
   c.tok = kChunkRows / (s->hq / s->hkv);
   c.units = (int64_t)s->n_tokens / c.tok + s->nseq;
+  // no more workgroups than there can be shares: what the table, or the window, lets a unit see at most  (16 tokens behind 4080 keys: 22.7 us, with all of them 23.3)
+  int64_t pieces = ((int64_t)s->max_pages * s->page + 63) / 64;
+  if (window_of(s) > 0 && pieces > (window_of(s) + c.tok) / 64 + 2) pieces = (window_of(s) + c.tok) / 64 + 2;
+  const int64_t shares = c.units < 64 * kSlots ? (c.units * s->hkv * (kUnitCost + pieces) + kLeastShare - 1) / kLeastShare : kSlots;
+  c.slots = shares < kSlots ? (int)((shares + 7) & ~(int64_t)7) : kSlots;
   c.ml = (size_t)2 * kSlots * kChunkRows * kD * 4;
   c.joints = c.ml + (size_t)2 * kSlots * kChunkRows * 8;
   c.total = c.joints + kSlots * sizeof(Joint);
@@ -967,6 +973,7 @@ int nsa_sel_cache_attention_chunk(const nsa_sel_cache_shape* shape, const void* 
   A.tok = c.tok;
   A.g_magic = C.g == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / (uint32_t)C.g + 1);
   A.units = (int32_t)c.units;
+  A.slots = c.slots;
   A.part = (float*)ws;
   A.part_ml = (float2*)((char*)ws + c.ml);
   A.joints = (Joint*)((char*)ws + c.joints);
@@ -976,11 +983,11 @@ int nsa_sel_cache_attention_chunk(const nsa_sel_cache_shape* shape, const void* 
   if (allow_dynamic_lds((const void*)kern, kChunkLds, ready[e4m3]) != hipSuccess) return NSA_SEL_EHIP;
   {
     ProfScope ps(KID_CACHE_CHUNK, (hipStream_t)stream);
-    hipLaunchKernelGGL(kern, dim3(kSlots), dim3(kChunkThreads), kChunkLds, (hipStream_t)stream, Args{C, A});
+    hipLaunchKernelGGL(kern, dim3(c.slots), dim3(kChunkThreads), kChunkLds, (hipStream_t)stream, Args{C, A});
   }
   if (hipGetLastError() != hipSuccess) return NSA_SEL_EHIP;
   ProfScope ps(KID_CACHE_CHUNK_JOIN, (hipStream_t)stream);
-  hipLaunchKernelGGL(k_cache_chunk_join, dim3(8 * kSlots), dim3(kChunkJoinThreads), 0, (hipStream_t)stream, Args{C, A});
+  hipLaunchKernelGGL(k_cache_chunk_join, dim3(8 * c.slots), dim3(kChunkJoinThreads), 0, (hipStream_t)stream, Args{C, A});
   return hipGetLastError() == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP;
 }
 
