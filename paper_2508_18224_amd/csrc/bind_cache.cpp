@@ -6,6 +6,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
+#include <c10/core/AutogradState.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -39,12 +40,16 @@ const at::Tensor& dims(PyObject* o, const char* name, int64_t n) {
   return t;
 }
 
+// A tensor that carries a forward gradient, where those are on (with grad mode off too).
+bool has_tangent(const at::Tensor& t) { return c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined(); }
+
 void expect_kind(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape, const at::Device& dev) {
   if (t.scalar_type() != type) throw Refused{std::string(name) + " must be " + c10::toString(type) + ", got " + c10::toString(t.scalar_type())};
   if (t.sizes() != shape) throw Refused{std::string(name) + " must have shape " + text(shape) + ", got " + text(t.sizes())};
   if (t.device() != dev) throw Refused{std::string(name) + " must live on " + dev.str() + ", got " + t.device().str()};
   if (t.requires_grad() && at::GradMode::is_enabled())
     throw Refused{std::string(name) + " requires grad, and the calls over a cache have no backward: call under torch.no_grad(), or detach it"};
+  if (has_tangent(t)) throw Refused{std::string(name) + " has a forward gradient, which the calls down to the library would lose: detach it"};
 }
 // A contiguous tensor; its address.
 void* expect(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape, const at::Device& dev) {
@@ -372,7 +377,7 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = dims(a[0], "scores", 3);
     const at::Device dev = x.device();
     const int64_t T = x.size(0), hkv = x.size(1), stride = x.size(2);
-    const void* scores = expect(x.requires_grad() ? x.detach() : x, "scores", at::kFloat, x.sizes(), dev);  // block ids have no gradient
+    const void* scores = expect(x.requires_grad() || has_tangent(x) ? x.detach() : x, "scores", at::kFloat, x.sizes(), dev);  // block ids have no gradient
     const at::Tensor& lengths = dims(a[1], "kv_len", 1);
     const int64_t nseq = lengths.size(0);
     if (T > INT32_MAX || hkv > INT32_MAX || nseq > INT32_MAX) throw Refused{"too many tokens, heads or sequences"};
@@ -660,6 +665,8 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Turn how = {dims(a[2], "inv_freq", 1), maybe(a[3], "cu_seqlens", 1), maybe(a[4], "positions", 1), truth(a[5]), truth(a[7]), PyFloat_AsDouble(a[6]), PyLong_AsVoidPtr(a[11])};
     if (PyErr_Occurred()) throw python_error();
     if (truth(a[10])) {
+      for (int i = 0; i < 2; ++i)
+        if (x[i].defined() && has_tangent(x[i])) throw Refused{std::string(i == 0 ? "q" : "k") + " has a forward gradient, and the rotation has a backward one only: detach it"};
       if (how.inv_freq.requires_grad()) throw Refused{"inv_freq requires grad, and the rotation has a gradient for q and k only: detach it"};
       without_gil([&] {
         auto r = Rotation::of(x[0], x[1], how);
