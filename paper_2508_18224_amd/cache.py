@@ -27,7 +27,7 @@ class PagedCache:
 
     A piece of a prompt is append and attention_chunk; read gives keys and values back as rows.
 
-    Forward only: in grad mode tensors that require grad are refused, and tensors with a forward gradient.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
+    Forward only: in grad mode tensors that require grad are refused, and tensors with a forward gradient; no call can be traced.  Calls keep nothing between them and may run on any stream and be captured; calls that write the same pages at once
     race, as writes to any tensor do.
 
     k_pages, v_pages, k_scale, v_scale (None in bfloat16), n_pages, hkv, page and device are there to be read.  The tensors are looked at in every call:

@@ -7,9 +7,12 @@
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
 #include <c10/core/AutogradState.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <string>
 
@@ -107,6 +110,12 @@ void done(int rc, const char* what) {
 }
 void on_gpu(const at::Device& dev) {
   if (!dev.is_cuda()) throw Refused{"tensors must be contiguous device tensors"};
+}
+// A trace records what goes through torch's dispatcher, which here is the results' memory alone: what fills it would be lost.
+void not_traced() {
+  if (torch::jit::tracer::isTracing() || c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PreDispatch) ||
+      c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY).has_value())
+    throw Refused{"a call down to the library cannot be traced: a trace would not hold it"};
 }
 void count(Py_ssize_t got, Py_ssize_t want) {
   if (got != want) throw Refused{"internal: wrong number of arguments"};
@@ -233,6 +242,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     count(n, 13);
+    not_traced();
     const CacheInfo& c = info(a[0]);
     const Pages p = pages(c);
     const at::Tensor &k = dims(a[1], "k", 3), &v = dims(a[2], "v", 3);
@@ -299,6 +309,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     count(n, 15);
+    not_traced();
     const CacheInfo& c = info(a[0]);
     const Pages p = pages(c);
     const at::Tensor& q = dims(a[1], "q", 3);
@@ -374,6 +385,7 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     count(n, 9);
+    not_traced();
     const at::Tensor& x = dims(a[0], "scores", 3);
     const at::Device dev = x.device();
     const int64_t T = x.size(0), hkv = x.size(1), stride = x.size(2);
@@ -422,6 +434,7 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     count(n, 8);
+    not_traced();
     const CacheInfo& c = info(a[0]);
     const Pages p = pages(c);
     int64_t T = a[3] == Py_None ? dims(a[1], "table", 2).size(0) : -1;
@@ -471,6 +484,7 @@ PyObject* attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
     count(n, 13);
+    not_traced();
     const CacheInfo& c = info(a[0]);
     const Pages p = pages(c);
     const at::Tensor& q = dims(a[1], "q", 3);
@@ -543,6 +557,7 @@ struct Turn {
 };
 // x[0] and, if it is defined, x[1], turned into y (made where it is undefined).  No Python here: the gradient's thread calls it too.
 void rotate(const at::Tensor (&x)[2], at::Tensor (&y)[2], const Turn& how) {
+  not_traced();
   nsa_sel_rotary_shape s = {};
   const void* in[2] = {nullptr, nullptr};
   void* out[2] = {nullptr, nullptr};

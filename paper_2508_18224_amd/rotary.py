@@ -13,7 +13,7 @@ from .binding import NsaSelError, call_native, native
 def rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
            positions: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
            k_out: Optional[torch.Tensor] = None):
-    """(q, k) turned by their tokens' places; differentiable in q and k (backward; tensors with a forward gradient are refused).  q, k: bfloat16 [tokens, heads, 128] device tensors, any numbers of heads, that may be slices
+    """(q, k) turned by their tokens' places; differentiable in q and k (backward; tensors with a forward gradient and tracing are refused).  q, k: bfloat16 [tokens, heads, 128] device tensors, any numbers of heads, that may be slices
     whose tokens lie apart (k may be None).  With factor 1 the bits are those that PagedCache.append writes.
 
     inv_freq: float64 [rot / 2], radians per place, rot a multiple of 16 up to 128 leading channels, and factor, which multiplies those channels: rotary_frequencies gives both.
