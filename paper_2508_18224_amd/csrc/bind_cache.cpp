@@ -236,6 +236,13 @@ PyObject* given(PyObject* o) {
   Py_INCREF(o);
   return o;
 }
+// A tensor of the caller's that the library has written: a backward pass that saved what was there finds out by its version (tensors of inference mode have none).
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(PyObject* o) {
+  if (o != Py_None) written(THPVariable_Unpack(o));
+}
 
 // (info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out, stream) -> (rotated q or None, rotated k or None)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -292,6 +299,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                        (int32_t)(2 * pairs), interleaved, p.k, p.v, p.ks, p.vs, q_out, k_out, stream);
          }),
          "nsa_sel_cache_append");
+    for (const at::Tensor& t : c.t)
+      if (t.defined()) written(t);
+    written(a[10]);
+    written(a[11]);
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
     PyTuple_SET_ITEM(r, 0, new_q.defined() ? THPVariable_Wrap(std::move(new_q)) : given(a[6] == Py_None ? Py_None : a[10]));
@@ -368,6 +379,8 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
            return nsa_sel_cache_attention(&s, q_ptr, idx, b.cu, b.kv_len, b.table, p.k, p.v, p.ks, p.vs, gate, acc, out, (float*)lse, ws, need, stream);
          }),
          "nsa_sel_cache_attention");
+    written(a[11]);
+    written(a[12]);
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
     PyTuple_SET_ITEM(r, 0, new_o.defined() ? THPVariable_Wrap(std::move(new_o)) : given(a[11]));
@@ -421,6 +434,7 @@ PyObject* select_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
            return nsa_sel_select_blocks_cached(&s, (const float*)scores, stride, cu, (const int32_t*)kv_len, n_sink, n_local, (int32_t*)out, queue);
          }),
          "nsa_sel_select_blocks_cached");
+    written(a[7]);
     return made.defined() ? THPVariable_Wrap(std::move(made)) : given(a[7]);
   } catch (const Refused& r) {
     PyErr_SetString(g_error, r.why.c_str());
@@ -468,6 +482,8 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* const stream = PyLong_AsVoidPtr(a[7]);
     done(without_gil([&] { return nsa_sel_cache_read(&s, b.cu, b.kv_len, b.table, p.k, p.v, p.ks, p.vs, out[0], stride[0], out[1], stride[1], stream); }),
          "nsa_sel_cache_read");
+    written(a[5]);
+    written(a[6]);
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
     for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(r, i, made[i].defined() ? THPVariable_Wrap(std::move(made[i])) : given(a[5 + i]));
@@ -535,6 +551,8 @@ PyObject* attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
            return nsa_sel_cache_attention_chunk(&s, q_ptr, b.cu, b.kv_len, b.table, p.k, p.v, p.ks, p.vs, gate, acc, out, (float*)lse, ws, need, stream);
          }),
          "nsa_sel_cache_attention_chunk");
+    written(a[9]);
+    written(a[10]);
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
     PyTuple_SET_ITEM(r, 0, new_o.defined() ? THPVariable_Wrap(std::move(new_o)) : given(a[9]));
@@ -689,6 +707,8 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
       });
     } else {
       without_gil([&] { rotate(x, y, how); });
+      written(a[8]);
+      written(a[9]);
     }
     PyObject* r = PyTuple_New(2);
     if (!r) throw python_error();
