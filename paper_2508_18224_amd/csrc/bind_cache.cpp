@@ -628,12 +628,13 @@ void rotate(const at::Tensor (&x)[2], at::Tensor (&y)[2], const Turn& how) {
   done(nsa_sel_rotary(&s, in[0], from[0], in[1], from[1], (const int32_t*)cu, (const int32_t*)positions, freq, out[0], to[0], out[1], to[1], how.stream), "nsa_sel_rotary");
 }
 
-// A gradient as the library takes rows: gradients come as the graph made them, expanded, transposed.
+// A gradient as the library takes rows: gradients come as the graph made them, expanded, transposed, out of the middle of a buffer.  (A copy where contiguous() would be none: a slice that is
+// contiguous, at an address that is not aligned.)
 at::Tensor rows_of(const at::Tensor& x) {
   const int64_t T = x.size(0), h = x.size(1);
   const bool fits = x.stride(2) == 1 && (h == 1 || x.stride(1) == kD) && (T == 1 || (x.stride(0) >= h * kD && x.stride(0) % 8 == 0)) &&
                     (reinterpret_cast<uintptr_t>(x.data_ptr()) & 15) == 0;
-  return fits ? x : x.contiguous();
+  return fits ? x : x.clone(at::MemoryFormat::Contiguous);
 }
 
 // The gradient of a rotation is the rotation back, a node of the same kind, which makes it differentiable itself.  In C++ since the engine then needs no Python: a pass forward and back over
