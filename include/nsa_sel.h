@@ -253,6 +253,13 @@ int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_
                          const int32_t* table, const double* inv_freq, int32_t rot, int32_t interleaved, void* k_pages,
                          void* v_pages, float* k_scale, float* v_scale, void* Q_out, void* K_out, void* stream);
 
+/* The same with a factor of the channels that turn, of queries and keys, as nsa_sel_rotary has it (<= 0 selects 1): the append of a model whose frequencies were changed
+ * for a longer context together with one. */
+int nsa_sel_cache_append_factor(const nsa_sel_cache_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                                const void* V, int64_t v_stride, const int32_t* cu_seqlens, const int32_t* kv_len,
+                                const int32_t* table, const double* inv_freq, int32_t rot, int32_t interleaved, double factor, void* k_pages,
+                                void* v_pages, float* k_scale, float* v_scale, void* Q_out, void* K_out, void* stream);
+
 /* Bytes of the workspace of nsa_sel_cache_attention for `shape` (0 where the call needs none). */
 int nsa_sel_cache_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes);
 
@@ -298,7 +305,7 @@ int nsa_sel_select_blocks_cached(const nsa_sel_cache_shape* shape, const float* 
                                  int32_t* idx, void* stream);
 
 /* ---- rotary positions ------------------------------------------------------------------------------------------------
- * Queries and keys of a packed batch turned by their places, as nsa_sel_cache_append turns them on the way to a cache (with factor 1 bit for bit), for the
+ * Queries and keys of a packed batch turned by their places, as nsa_sel_cache_append and nsa_sel_cache_append_factor turn them on the way to a cache (bit for bit), for the
  * training path: Q_out, K_out [n_tokens, heads, d] bf16 from Q, K.  Pair i of a row at place p, channels a and b, becomes
  * factor * (x_a cos - x_b sin), factor * (x_b cos + x_a sin) of the angle p * inv_freq[i]; the channels from rot on are copied.  The gradient of this
  * is the same call with inverse != 0 on the gradients of the results.

@@ -12,7 +12,7 @@ _LIB_PATH = os.path.join(_HERE, "libnsa_sel.so")
 _lib = None
 
 SYMBOLS = ["nsa_sel_workspace_bytes", "nsa_sel_workspace_bytes_min", "nsa_sel_build_index", "nsa_sel_index_view", "nsa_sel_fwd", "nsa_sel_bwd", "nsa_sel_fwd_static", "nsa_sel_fwd_query_outer", "nsa_sel_fwd_gated", "nsa_sel_bwd_gated", "nsa_sel_select_blocks",
-           "nsa_sel_cache_append", "nsa_sel_cache_workspace_bytes", "nsa_sel_cache_attention", "nsa_sel_select_blocks_cached",
+           "nsa_sel_cache_append", "nsa_sel_cache_append_factor", "nsa_sel_cache_workspace_bytes", "nsa_sel_cache_attention", "nsa_sel_select_blocks_cached",
            "nsa_sel_cache_chunk_workspace_bytes", "nsa_sel_cache_attention_chunk", "nsa_sel_cache_read", "nsa_sel_rotary",
            "nsa_sel_profile_enable", "nsa_sel_profile_select", "nsa_sel_profile_collect", "nsa_sel_calibration_copy", "nsa_sel_mfma_probe", "nsa_sel_strerror"]
 
@@ -60,6 +60,7 @@ def lib():
         L.nsa_sel_select_blocks.argtypes = [C.POINTER(Shape), vp, C.c_int64, i32p, C.c_int32, C.c_int32, i32p, vp]
         i64 = C.c_int64
         L.nsa_sel_cache_append.argtypes = [C.POINTER(CacheShape), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, vp]
+        L.nsa_sel_cache_append_factor.argtypes = [C.POINTER(CacheShape), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_double, vp, vp, vp, vp, vp, vp, vp]
         L.nsa_sel_cache_workspace_bytes.argtypes = [C.POINTER(CacheShape), C.POINTER(sz)]
         L.nsa_sel_cache_attention.argtypes = [C.POINTER(CacheShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.nsa_sel_select_blocks_cached.argtypes = [C.POINTER(CacheShape), vp, i64, vp, vp, C.c_int32, C.c_int32, vp, vp]

@@ -69,17 +69,18 @@ class PagedCache:
     device = property(lambda self: self._device)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *,
-               q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+               q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0,
                rotated_k: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """Writes k and v (bfloat16 [tokens, hkv, 128]) to the pages, k rotated by its tokens' places, and returns (rotated q or None,
         rotated k as bfloat16 or None).  q, k, v may be slices whose tokens lie apart.
 
         inv_freq: float64 [rot / 2], radians per place, rot a multiple of 16 up to 128 leading channels; None rotates nothing.  Pairs are
-        channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved.  rotated_k also returns the rotated keys, for the prompt's own
+        channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved.  factor multiplies the channels that turn, of q and k: rotary_frequencies gives it with
+        frequencies that need one.  rotated_k also returns the rotated keys, for the prompt's own
         attention.  q_out / k_out take the results (they may be q / k themselves if those are contiguous); rows of tokens that belong to no
         sequence, and of tokens of negative place (idle slots, with kv_len 0), are left as they are there, and uninitialised otherwise: attention looks at
         neither."""
-        return call_native(self._calls.append, self._device, self._info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out)
+        return call_native(self._calls.append, self._device, self._info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out, factor)
 
     def workspace_bytes(self, tokens: int, hq: int, nseq: int, max_pages: int, *, topk: int = 0, block: int = 64, window: int = 0) -> int:
         """Bytes that attention() of such a call needs as `ws`."""

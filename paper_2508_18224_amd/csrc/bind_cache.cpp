@@ -90,6 +90,12 @@ float number(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw python_error();
   return (float)v;
 }
+double factor_of(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw python_error();
+  if (!(v > 0.0)) throw Refused{"factor must be positive"};
+  return v;
+}
 
 // Other Python threads run while torch allocates and the library launches: the allocator may wait, and so may a full queue.
 struct WithoutGil {
@@ -244,11 +250,11 @@ void written(PyObject* o) {
   if (o != Py_None) written(THPVariable_Unpack(o));
 }
 
-// (info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out, stream) -> (rotated q or None, rotated k or None)
+// (info, k, v, table, kv_len, cu, q, inv_freq, interleaved, rotated_k, q_out, k_out, factor, stream) -> (rotated q or None, rotated k or None)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    count(n, 13);
+    count(n, 14);
     not_traced();
     const CacheInfo& c = info(a[0]);
     const Pages p = pages(c);
@@ -291,12 +297,13 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (pairs > kD) throw Refused{"inv_freq must be float64 [rot / 2], rot a multiple of 16 up to 128"};
     }
     const nsa_sel_cache_shape s = shape_of(c, b, T, hq);
+    const double factor = factor_of(a[12]);
     on_gpu(c.device);
     const bool interleaved = truth(a[8]);
-    void* const stream = PyLong_AsVoidPtr(a[12]);
+    void* const stream = PyLong_AsVoidPtr(a[13]);
     done(without_gil([&] {
-           return nsa_sel_cache_append(&s, q_ptr, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, b.cu, b.kv_len, b.table, freq,
-                                       (int32_t)(2 * pairs), interleaved, p.k, p.v, p.ks, p.vs, q_out, k_out, stream);
+           return nsa_sel_cache_append_factor(&s, q_ptr, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, b.cu, b.kv_len, b.table, freq,
+                                       (int32_t)(2 * pairs), interleaved, factor, p.k, p.v, p.ks, p.vs, q_out, k_out, stream);
          }),
          "nsa_sel_cache_append");
     for (const at::Tensor& t : c.t)
@@ -565,7 +572,6 @@ PyObject* attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// (q, k, inv_freq, cu, positions, interleaved, factor, inverse, q_out, k_out, stream) -> (rotated q, rotated k or None)
 // ---- the rotation: of tensors, as a node of a graph, and from Python ----------------------------------------------------------------
 struct Turn {
   at::Tensor inv_freq, cu, positions;  // the last two may be undefined

@@ -23,7 +23,7 @@ constexpr int kAttendThreads = 256, kJoinThreads = 256;
 
 // Returns a status of the C ABI.
 int launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
-                               const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, void* Q_out,
+                               const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, double factor, void* Q_out,
                                void* K_out, hipStream_t st);
 
 // What the attention of a call reads besides the cache, and where its results go.

@@ -83,13 +83,13 @@ using namespace nsa;
 
 extern "C" {
 
-int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
-                         const void* V, int64_t v_stride, const int32_t* cu_seqlens, const int32_t* kv_len,
-                         const int32_t* table, const double* inv_freq, int32_t rot, int32_t interleaved, void* k_pages,
-                         void* v_pages, float* k_scale, float* v_scale, void* Q_out, void* K_out, void* stream) {
+int nsa_sel_cache_append_factor(const nsa_sel_cache_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                                const void* V, int64_t v_stride, const int32_t* cu_seqlens, const int32_t* kv_len,
+                                const int32_t* table, const double* inv_freq, int32_t rot, int32_t interleaved, double factor, void* k_pages,
+                                void* v_pages, float* k_scale, float* v_scale, void* Q_out, void* K_out, void* stream) {
   int rc = check_cache_shape(shape, false);
   if (rc) return rc;
-  if (rot < 0 || rot > kD || (rot & 15) != 0) return NSA_SEL_EINVAL;
+  if (rot < 0 || rot > kD || (rot & 15) != 0 || !(factor < __builtin_inf())) return NSA_SEL_EINVAL;
   if (shape->n_tokens == 0) return NSA_SEL_OK;
   rc = check_cache_pointers(shape, k_pages, v_pages, k_scale, v_scale, table, kv_len, cu_seqlens);
   if (rc) return rc;
@@ -102,7 +102,15 @@ int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_
   if (2 * units * shape->hkv + shape->n_tokens >= ((int64_t)1 << 31)) return NSA_SEL_EUNSUPPORTED;  // workgroups
   const Cache C = make_cache(shape, k_pages, v_pages, k_scale, v_scale, table, kv_len, cu_seqlens);
   return launch_cache_append(C, shape->dtype == NSA_SEL_CACHE_E4M3, Q, q_stride, K, k_stride, V, v_stride, inv_freq, rot,
-                             interleaved != 0, Q_out, K_out, (hipStream_t)stream);
+                             interleaved != 0, factor > 0.0 ? factor : 1.0, Q_out, K_out, (hipStream_t)stream);
+}
+
+int nsa_sel_cache_append(const nsa_sel_cache_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                         const void* V, int64_t v_stride, const int32_t* cu_seqlens, const int32_t* kv_len,
+                         const int32_t* table, const double* inv_freq, int32_t rot, int32_t interleaved, void* k_pages,
+                         void* v_pages, float* k_scale, float* v_scale, void* Q_out, void* K_out, void* stream) {
+  return nsa_sel_cache_append_factor(shape, Q, q_stride, K, k_stride, V, v_stride, cu_seqlens, kv_len, table, inv_freq, rot, interleaved, 1.0, k_pages, v_pages,
+                                     k_scale, v_scale, Q_out, K_out, stream);
 }
 
 int nsa_sel_cache_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes) {

@@ -44,7 +44,7 @@ __device__ __forceinline__ void token_rows(const Cache& C, const AppendArgs& A, 
     if constexpr (kStore) L.page[wave] = place < 0 ? -1 : page_of(C, P.s, place);
     for (int i = threadIdx.x & 63; i < A.R.rot >> 1; i += 64) {
       const double2 x = cos_sin(place, A.R.inv_freq[i]);
-      L.cs[wave * kMaxPairs + place_of_pair(A.R, i)] = float2{(float)x.x, (float)x.y};
+      L.cs[wave * kMaxPairs + place_of_pair(A.R, i)] = float2{(float)(x.x * A.R.factor), (float)(x.y * A.R.factor)};
     }
   }
   const int sub = threadIdx.x & 15, nq = A.Q ? C.hq : 0, each = nq + (kStore ? 2 * C.hkv : 0), rows = min(kTokens, C.T - t0) * each;
@@ -193,7 +193,7 @@ __device__ __forceinline__ void page_rows(const Cache& C, const AppendArgs& A, c
         const int p = k & (kMaxPairs - 1), row = k / kMaxPairs;
         if (p < A.R.rot >> 1) {
           const double2 t = cos_sin(U.first + tile * kTileRows + row, A.R.inv_freq[p]);
-          cs[row * kMaxPairs + place_of_pair(A.R, p)] = float2{(float)t.x, (float)t.y};
+          cs[row * kMaxPairs + place_of_pair(A.R, p)] = float2{(float)(t.x * A.R.factor), (float)(t.y * A.R.factor)};
         }
       }
       __syncthreads();
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 64 ? 3 : 4) k_cache_appe
 }  // namespace
 
 int launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
-                        const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, void* Q_out,
+                        const void* V, int64_t v_stride, const double* inv_freq, int rot, bool interleaved, double factor, void* Q_out,
                         void* K_out, hipStream_t st) {
   AppendArgs A;
   A.Q = (const bf16_t*)Q;
@@ -329,6 +329,7 @@ int launch_cache_append(const Cache& C, bool e4m3, const void* Q, int64_t q_stri
   A.R.inv_freq = inv_freq;
   A.R.rot = rot;
   A.R.interleaved = interleaved ? 1 : 0;
+  A.R.factor = factor;
   const int each = (Q ? C.hq : 0) + (e4m3 ? 0 : 2 * C.hkv);
   auto status = [] { return hipGetLastError() == hipSuccess ? NSA_SEL_OK : NSA_SEL_EHIP; };
   auto groups = [&](int tokens) { return ((int64_t)C.T + tokens - 1) / tokens; };

@@ -21,7 +21,6 @@ struct RotaryArgs {
   const int32_t *cu, *positions;
   int32_t T, nseq, hq, each, tokens;  // each: rows of a token; tokens: of a workgroup
   uint32_t each_magic;                // see div_g
-  double factor;
   bool inverse;
   Rotation R;
 };
@@ -68,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) k_rotary(RotaryArgs A) {
         if ((threadIdx.x & 63) == 0) turns[k] = on;
         for (int i = threadIdx.x & 63; i < A.R.rot >> 1; i += 64) {
           const double2 c = cos_sin(place, A.R.inv_freq[i]);
-          cs[k * kMaxPairs + place_of_pair(A.R, i)] = float2{(float)(c.x * A.factor), (float)((A.inverse ? -c.y : c.y) * A.factor)};
+          cs[k * kMaxPairs + place_of_pair(A.R, i)] = float2{(float)(c.x * A.R.factor), (float)((A.inverse ? -c.y : c.y) * A.R.factor)};
         }
       }
       __syncthreads();
@@ -129,11 +128,11 @@ extern "C" int nsa_sel_rotary(const nsa_sel_rotary_shape* shape, const void* Q, 
   A.each_magic = A.each == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / (uint32_t)A.each + 1);
   const int want = kAtOnce * kBatch / A.each;
   A.tokens = want < 1 ? 1 : want > kMostTokens ? kMostTokens : want;
-  A.factor = s->factor > 0.0 ? s->factor : 1.0;
   A.inverse = s->inverse != 0;
   A.R.inv_freq = inv_freq;
   A.R.rot = s->rot;
   A.R.interleaved = s->interleaved != 0;
+  A.R.factor = s->factor > 0.0 ? s->factor : 1.0;
   const int64_t groups = ((int64_t)A.T + A.tokens - 1) / A.tokens;
   if (!launchable(groups, kThreads)) return NSA_SEL_EUNSUPPORTED;
   ProfScope ps(KID_ROTARY, (hipStream_t)stream);

@@ -1,5 +1,5 @@
 // Rotation by the place p, as the append to a cache (cache_append.hip) and the rotation by itself (rotary.hip) do it, bit for bit alike: channels a, b of
-// a pair i become  x_a cos(p f_i) - x_b sin(p f_i),  x_b cos(p f_i) + x_a sin(p f_i).  The angle is formed in 64 bits, in turns, less its nearest whole
+// a pair i become  x_a cos(p f_i) - x_b sin(p f_i),  x_b cos(p f_i) + x_a sin(p f_i), times a factor that cosine and sine have before they are rounded.  The angle is formed in 64 bits, in turns, less its nearest whole
 // number, so that a place of 2^20 loses nothing; its sine and cosine are worked out in 64 bits too and rounded to 32, in which the rest is
 // done.  Each product is rounded by itself, not fused into the sum, so that a value next to the border of two e4m3 values is stored
 // as elementary 32-bit operations put it.
@@ -14,6 +14,7 @@ struct Rotation {
   const double* inv_freq;  // [rot / 2], radians per place
   int32_t rot;             // channels that turn, a multiple of 16
   int32_t interleaved;     // pairs (2 i, 2 i + 1); else (i, i + rot / 2)
+  double factor;           // of the channels that turn
 };
 
 #if defined(__HIPCC__)

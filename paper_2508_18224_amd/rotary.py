@@ -14,7 +14,7 @@ def rotary(q: torch.Tensor, k: Optional[torch.Tensor], inv_freq: torch.Tensor, c
            positions: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0, q_out: Optional[torch.Tensor] = None,
            k_out: Optional[torch.Tensor] = None):
     """(q, k) turned by their tokens' places; differentiable in q and k (backward; tensors with a forward gradient and tracing are refused).  q, k: bfloat16 [tokens, heads, 128] device tensors, any numbers of heads, that may be slices
-    whose tokens lie apart (k may be None).  With factor 1 the bits are those that PagedCache.append writes.
+    whose tokens lie apart (k may be None).  The bits are those that PagedCache.append writes.
 
     inv_freq: float64 [rot / 2], radians per place, rot a multiple of 16 up to 128 leading channels, and factor, which multiplies those channels: rotary_frequencies gives both.
     Pairs are channels (i, i + rot / 2), or (2 i, 2 i + 1) if interleaved.  The place of a token is its place in its sequence by cu (int32 [sequences + 1]; None: one
