@@ -60,7 +60,12 @@ inline int check_cache_pointers(const nsa_sel_cache_shape* s, const void* k, con
 // Lengths below this one are this one: places that follow from them are negative all the same, and no sum leaves 32 bits.
 constexpr int kLeastLength = -(1 << 30);
 
-// No place is as far back as 2^30 of another: a window that long is none, and the kernels' sums with one stay in 32 bits.
+// The first place that a window shows to the token at `place`, 0 or more, for every place and window: the difference of those far apart is not formed.
+constexpr int32_t window_start(int32_t place, int32_t window) { return place >= window ? place + 1 - window : 0; }
+static_assert(window_start(INT32_MIN, INT32_MAX) == 0 && window_start(kLeastLength - (1 << 20), (1 << 30) - 1) == 0);
+static_assert(window_start(INT32_MAX - 1, 1) == INT32_MAX - 1 && window_start(5, 6) == 0 && window_start(6, 6) == 1 && window_start(7, 6) == 2);
+
+// No place is as far back as 2^30 of another: a window that long is none, and the kernels' sums of one with a place from -2^30 on stay in 32 bits.
 inline int32_t window_of(const nsa_sel_cache_shape* s) { return s->window < (1 << 30) ? s->window : 0; }
 
 }  // namespace nsa

@@ -10,7 +10,7 @@
 // 1.0 ms by card, 1.13 to 1.2 PFLOP/s; a large library product reaches 1.6.
 //
 // A page of 16 tokens or more is a run of memory, so the eight rows that a wavefront moves of a piece's K and V are always one page's: which one is looked up for 64 pieces
-// at a time, a piece a lane.
+// at a time, a piece a lane, and in the loop, which asks three pieces ahead, again after 61.
 //
 // Probabilities are rounded to bf16 for their product, as in the prompt's own attention (their relative error counts, and is the same for all of them); the sums they are
 // divided by are not.
@@ -45,10 +45,10 @@ struct ChunkArgs {
   uint32_t g_magic;  // see div_g
   int32_t units;     // of a KV head, at most
   int32_t slots;     // workgroups, a multiple of 8
-  // parts of units: slot 2 w of workgroup w for the unit that others begin, 2 w + 1 for the one that it begins and others finish
-  float* part;       // [slots][8 wavefronts][16][64 lanes][4]: the sums as the lanes hold them
-  float2* part_ml;   // [slots][256] (reference, sum)
-  struct Joint* joints;
+  // parts of units: part 2 w of workgroup w for the unit that others begin, 2 w + 1 for the one that it begins and others finish
+  float* part;       // [2 slots][8 wavefronts][16][64 lanes][4]: the sums as the lanes hold them
+  float2* part_ml;   // [2 slots][256] (reference, sum)
+  struct Joint* joints;  // [slots]
 };
 
 // A kernel's arguments, read anew from where the launch put them wherever this is called: held in registers through the loop over the keys, they would crowd out what that needs.
@@ -89,7 +89,7 @@ __device__ __forceinline__ Unit unit_of(const Cache& C, const ChunkArgs& A, int 
 }
 // The pieces that anything of the unit sees: [first, first + count).
 __device__ __forceinline__ int2 pieces_of(const Cache& C, const ChunkArgs& A, const Unit& W) {
-  const int hi = min(W.place + W.nt, C.max_pages << C.page_log2), lo = A.window > 0 ? max(W.place + 1 - A.window, 0) : 0;
+  const int hi = min(W.place + W.nt, C.max_pages << C.page_log2), lo = A.window > 0 ? window_start(W.place, A.window) : 0;
   const int first = lo / 64;
   return {first, max((hi + 63) / 64 - first, 0)};
 }
@@ -271,7 +271,7 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
     first = pieces_of(C, A, W).x + P.begin;
     wave_on = 32 * wave < rows;
     least_hi = min(W.place + div_g(min(32 * wave, rows - 1), C.g, A.g_magic) + 1, limit);
-    most_lo = A.window > 0 ? max(W.place + div_g(min(32 * wave + 31, rows - 1), C.g, A.g_magic) + 1 - A.window, 0) : 0;
+    most_lo = A.window > 0 ? window_start(W.place + div_g(min(32 * wave + 31, rows - 1), C.g, A.g_magic), A.window) : 0;
     c2 = A.scale * 1.4426950408889634f;
     k_base = C.k;
     v_base = C.v;
