@@ -919,7 +919,9 @@ ChunkCut chunk_cut(const nsa_sel_cache_shape* s) {
   // no more workgroups than there can be shares: what the table, or the window, lets a unit see at most  (16 tokens behind 4080 keys: 22.7 us, with all of them 23.3)
   int64_t pieces = ((int64_t)s->max_pages * s->page + 63) / 64;
   if (window_of(s) > 0 && pieces > (window_of(s) + c.tok) / 64 + 2) pieces = (window_of(s) + c.tok) / 64 + 2;
-  const int64_t shares = c.units < 64 * kSlots ? (c.units * s->hkv * (kUnitCost + pieces) + kLeastShare - 1) / kLeastShare : kSlots;
+  const int64_t rows = c.units * s->hkv;  // a unit of a head is a share at least
+  static_assert(kUnitCost >= kLeastShare);
+  const int64_t shares = rows < kSlots ? (rows * (kUnitCost + pieces) + kLeastShare - 1) / kLeastShare : kSlots;
   c.slots = shares < kSlots ? (int)((shares + 7) & ~(int64_t)7) : kSlots;
   c.ml = (size_t)2 * kSlots * kChunkRows * kD * 4;
   c.joints = c.ml + (size_t)2 * kSlots * kChunkRows * 8;
