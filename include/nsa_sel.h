@@ -281,7 +281,8 @@ int nsa_sel_cache_attention(const nsa_sel_cache_shape* shape, const void* Q, con
 int nsa_sel_cache_chunk_workspace_bytes(const nsa_sel_cache_shape* shape, size_t* bytes);
 
 /* nsa_sel_cache_attention for pieces of prompts: the same result (topk must be 0: every key, or a window) for many new tokens of a sequence, which share what they read of it:
- * up to 256 / g tokens at a time, where the call above shares among 16 / g.  Right for any number of new tokens, faster from 8 of them on behind 32768 keys, from 32 behind 4096.  A probability is rounded to
+ * up to 256 / g tokens at a time, where the call above shares among 16 / g.  Right for any number of new tokens.  Faster (32 query heads over 8, bf16) from 8 of them on
+ * behind 32768 keys; behind 4096 from 64 of one sequence, or from 16 of each of 16 sequences; from half as many with 64 query heads.  A probability is rounded to
  * bf16 for its product with the values, as in nsa_sel_fwd, where the call above gives it 16 bits.
  * The same call gives the same bits; how the keys are shared among workgroups follows from the batch, so that a token's last bits may differ between batches. */
 int nsa_sel_cache_attention_chunk(const nsa_sel_cache_shape* shape, const void* Q, const int32_t* cu_seqlens, const int32_t* kv_len,

@@ -118,7 +118,8 @@ class PagedCache:
                         scale: float = 0.0, gate: Optional[torch.Tensor] = None, o_acc: Optional[torch.Tensor] = None,
                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
         """(O, LSE) as attention() without `idx`, for pieces of prompts: up to 256 / g new tokens of a sequence (g = hq / hkv) share what they read of it.  Right for any
-        numbers of new tokens, faster than attention() from about 8 of a sequence on behind 32768 keys, from about 32 behind 4096; a probability has 8 bits in its product, there 16.  The arguments are those of attention(); ws is of chunk_workspace_bytes()."""
+        numbers of new tokens, faster than attention() (32 query heads over 8, bf16) from about 8 of a sequence on behind 32768 keys; behind 4096 from 64 of one sequence, or from 16
+        of each of 16 sequences; from half as many with 64 query heads.  A probability has 8 bits in its product, there 16.  The arguments are those of attention(); ws is of chunk_workspace_bytes()."""
         return call_native(self._calls.attention_chunk, self._device, self._info, q, table, kv_len, cu, window, scale, gate, o_acc, out, lse, ws)
 
     def read(self, table: torch.Tensor, kv_len: torch.Tensor, cu: Optional[torch.Tensor] = None, *, tokens: Optional[int] = None,

@@ -5,9 +5,9 @@
 // SIMD, each with its Q and its output in registers, share a piece's K and V in LDS.  A piece is 32 KB and 8.4 MFLOP, 2048 clocks of the matrix pipes; reading its operands takes the
 // LDS as long.
 //
-// What bounds it is the vector phase, and power: a wavefront's vector phase takes 1760 clocks, its matrix phase, beside another's vector phase, 1500, both together 3570, at 2.0 to 2.1 GHz
-// with random numbers.  (The products of a piece and their operand reads alone: 1.23 us, at 1.7 GHz; the whole: 1.68.)  2048 new tokens of 32 heads behind 32768 keys (8 KV heads) take 0.94 to
-// 1.0 ms by card, 1.13 to 1.2 PFLOP/s; a large library product reaches 1.6.
+// What bounds it is the vector phase, and power: a wavefront's vector phase takes 1810 clocks, its matrix phase, beside another's vector phase, 1610, both together 3880, at 2.0 to 2.1 GHz
+// with random numbers.  (The products of a piece and their operand reads alone: 1.23 us, at 1.7 GHz; the whole: 1.82.)  2048 new tokens of 32 heads behind 32768 keys (8 KV heads) take 0.99 to
+// 1.02 ms by card, 1.11 to 1.14 PFLOP/s; a large library product reaches 1.6.
 //
 // A page of 16 tokens or more is a run of memory, so the eight rows that a wavefront moves of a piece's K and V are always one page's: which one is looked up for 64 pieces
 // at a time, a piece a lane, and in the loop, which asks three pieces ahead, again after 61.
@@ -26,8 +26,8 @@ constexpr int kChunkWaves = 8, kChunkRows = 32 * kChunkWaves, kChunkThreads = 64
 constexpr int kStages = 4;  // tiles of K, and of V: one more than a piece that is asked for two before it is used needs, so that nobody waits for the tile to be free
 constexpr int kChunkV = kStages * kPieceBytes, kChunkLds = 2 * kStages * kPieceBytes + 64;
 constexpr int kSlots = 256;  // workgroups that share all units' pieces evenly, at most
-// What a unit costs beside its pieces, in pieces: its Q, its pages, the first and the last piece, its result, 10 to 12 us for 1.9 of a piece.  (A whole prompt of 8192 tokens: 1300 us
-// with none of it counted, 1023 with 5, 1004 with 6, 1013 with 8.)
+// What a unit costs beside its pieces, in pieces: its Q, its pages, the first and the last piece, its result, 10 to 12 us for 1.8 of a piece.  (A whole prompt of 8192 tokens: 1300 us
+// with none of it counted, 1023 with 5, 1004 with 6, 1013 with 8, when a piece took 1.7.)
 constexpr int kUnitCost = 6;
 constexpr int kLeastSpan = 2, kLeastShare = 6;  // (16 tokens behind 4080 keys: 23.6 us with 5 or 6 to a workgroup, 24.7 with 7, 28.5 with 12)
 constexpr int kChunkJoinThreads = 512;
@@ -419,7 +419,7 @@ __device__ __forceinline__ void attend_unit(Unit W, Span P, char* smem) {
     // A wavefront takes a matrix phase and a vector phase in turn: values of a piece and scores of the next, probabilities of those.  Of the two wavefronts of a SIMD one has the matrix
     // pipe while the other makes probabilities: a barrier after every phase keeps them so, the second half of the wavefronts a phase behind.  With the products of a piece (8 bits: in the
     // vector phase behind them) K of the third piece on and V of the second one on are asked for; they are there at the end of the next vector phase.  (One barrier for two pieces, a phase
-    // apart all the same: 3970 clocks a piece against 3640, and all eight in step 4180.  Asked for in the vector phase in 16 bits too: 1 % longer; maxima beside the products: 5 %.)
+    // apart all the same: 3970 clocks a piece where this took 3640, and all eight in step 4180.  Asked for in the vector phase in 16 bits too: 1 % longer; maxima beside the products: 5 %.)
     const bool behind = wave >= kChunkWaves / 2;
     auto tile = [](int step) { return (uint32_t)(step & (kStages - 1)) * kPieceBytes; };
     auto turn = [&]() __attribute__((always_inline)) {
